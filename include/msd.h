@@ -393,6 +393,75 @@ int msd_train_lr(int step, int total_steps, double lr_max, double* lr_out);
 int msd_train_mix(int epoch, int n_epochs, int n_per_epoch, int* n_text_out, int* n_visual_out);
 
 /*
+ * Microscaled 4-bit matrices and the operators on them.  They need no context:
+ * work is enqueued on `stream` (a hipStream_t of the current device; NULL = the
+ * null stream), nothing is allocated and nothing is waited for, so a call may be
+ * captured into a graph.  Calls on different streams or threads are independent.
+ * Errors: MSD_ERR_INVALID_ARG (then nothing was enqueued), MSD_ERR_HIP; the message
+ * is msd_last_error(NULL)'s on the calling thread.
+ *
+ * A row is cut into blocks of 32 values x that share a power of two,
+ * s = 2^(floor(log2 max|x|) - 2) within [2^-127, 2^127]; each value is held as
+ * x / s rounded to E2M1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), to the
+ * nearest, ties to the even code, 6 at most (MXFP4 of the OCP Microscaling Formats
+ * Specification v1.0).  A block with a NaN or an infinity stands for NaN in every
+ * place.  terms = 2 holds the blocks of x and those of what they leave of x (8 bits
+ * and two scales a value); the matrix stands for the sum.
+ *
+ * rows (0 .. 2^23) and cols (1 .. 2^20, any), rows * ceil(cols / 512) <= 2^25.
+ * layout: MSD_MX_ROWS, row by row (activations; terms 1 or 2), or MSD_MX_WEIGHT, the
+ * tiled layout that a product reads its weight in (terms 1).  codes_d and scales_d:
+ * 16-byte aligned device buffers of the sizes that msd_mx_bytes gives (it ignores
+ * both pointers); their contents are the library's own layout.  No buffer that a
+ * call writes may overlap another of its buffers unless the call says so.
+ *
+ * Float matrices are row-major [rows][cols] of `type`, their rows ld >= cols values
+ * apart (any; rows that are multiples of 16 bytes apart from a 16-byte aligned start
+ * move fastest).  Norm gains are bfloat16.
+ */
+enum { MSD_F32 = 0, MSD_BF16 = 1, MSD_F16 = 2 };
+enum { MSD_MX_ROWS = 0, MSD_MX_WEIGHT = 1 };
+typedef struct msd_mx {
+  void *codes_d, *scales_d;
+  int32_t rows, cols;
+  int32_t layout, terms;
+} msd_mx;
+
+/* Byte sizes of q's two buffers. */
+int msd_mx_bytes(const msd_mx* q, size_t* code_bytes, size_t* scale_bytes);
+
+/* q = the quantised src_d [q->rows][q->cols]. */
+int msd_mx_quantize(const void* src_d, int type, size_t ld, const msd_mx* q, void* stream);
+
+/* dst_d [q->rows][q->cols] = the values that q stands for, rounded once. */
+int msd_mx_dequantize(const msd_mx* q, void* dst_d, int type, size_t ld, void* stream);
+
+/*
+ * The residual's addition, its norm and the quantisation in one pass over the rows:
+ *   s = x + y (float32; y_d NULL: s = x),  sum_d = s rounded to `type` (unless NULL),
+ *   q = s / sqrt(mean(s^2) + eps) * gain, from s before that rounding.
+ * x_d, y_d and sum_d are of one type; sum_d may be x_d or y_d (with the same ld).  q: MSD_MX_ROWS,
+ * two terms, at most 8192 columns; eps >= 0 and finite.  A row of zeros with
+ * eps = 0 is NaN, as 0 / 0.
+ */
+int msd_mx_resid_norm(const void* x_d, size_t ldx, const void* y_d, size_t ldy, void* sum_d,
+                      size_t lds, int type, const void* gain_d, float eps, const msd_mx* q,
+                      void* stream);
+
+/* q = silu(gate) * up, silu(g) = g / (1 + e^-g) (float32).  q: MSD_MX_ROWS, two terms. */
+int msd_mx_swiglu(const void* gate_d, size_t ldg, const void* up_d, size_t ldu, int type,
+                  const msd_mx* q, void* stream);
+
+/*
+ * out_d[m][n] = sum over k of x[m][k] w[n][k], rounded once from float32 sums: x
+ * MSD_MX_ROWS (one or two terms), w MSD_MX_WEIGHT with the same cols, out_d
+ * [x->rows][w->rows] of `type`.  A call's result is the same every time.  At most
+ * 2^22 output tiles of 16 x 16.
+ */
+int msd_mx_product(const msd_mx* x, const msd_mx* w, void* out_d, int type, size_t ld,
+                   void* stream);
+
+/*
  * Diagnostic for measurement tools: one kernel that reads `bytes` of the
  * device buffer buf_d (16-byte aligned, zero-filled, bytes a multiple of
  * 64 KiB) with the access pattern of the library's weight stream (every wave

@@ -400,4 +400,37 @@ void tr_pack_t(const PackJobs& j, hipStream_t st);
 // the transpose of a row-major bf16 matrix [R][C], packed (one plane)
 void tr_pack_t16(const uint16_t* src, int R, int C, int Rp, uint16_t* dst, hipStream_t st);
 
+// ------------------------------------------------ microscaled 4 bits ----
+// A quantised matrix (formats and layouts: k_mx.hip).
+struct MxMat {
+  void *codes, *scales;
+  int rows, cols;
+  int terms;    // 1 or 2; a weight has 1
+  bool weight;  // the weight layout, else the rows layout
+};
+// Float types of the operators; as sources of a quantisation also a bf16 weight
+// in the packed layout (to the weight layout) and split rows (to the rows layout).
+enum { MX_F32 = 0, MX_BF16 = 1, MX_F16 = 2, MX_PACKED = 3, MX_SPLIT = 4 };
+inline int mx_tiles(int cols) { return (cols + 127) / 128; }
+inline int mx_groups(int cols) { return (cols + 511) / 512; }
+inline size_t mx_code_bytes(const MxMat& q) {
+  const size_t rows = q.weight ? ((size_t)q.rows + 15) / 16 * 16 : (size_t)q.rows;
+  return rows * q.terms * mx_tiles(q.cols) * 64;
+}
+inline size_t mx_scale_bytes(const MxMat& q) {
+  const size_t rows = q.weight ? ((size_t)q.rows + 15) / 16 * 16 : (size_t)q.rows;
+  return rows * q.terms * mx_groups(q.cols) * 16;
+}
+void launch_mx_quantise(const void* src, int type, size_t ld, const MxMat& q, hipStream_t st);
+void launch_mx_dequantise(const MxMat& q, void* dst, int type, size_t ld, hipStream_t st);
+// xo = x + y (when given), q = rmsnorm(x + y) * gain; y and xo may be null
+void launch_mx_norm(const void* x, size_t ldx, const void* y, size_t ldy, void* xo, size_t ldo,
+                    int type, const uint16_t* gain, float eps, const MxMat& q, hipStream_t st);
+// q = silu(gate) * up
+void launch_mx_swiglu(const void* gate, size_t ldg, const void* up, size_t ldu, int type,
+                      const MxMat& q, hipStream_t st);
+// out[m][n] = sum over k of x[m][k] w[n][k]
+void launch_mx_product(const MxMat& x, const MxMat& w, void* out, int type, size_t ldo,
+                       hipStream_t st);
+
 }  // namespace msd

@@ -15,6 +15,8 @@ MAX_TREE = 64
 
 MSD_OK, MSD_ERR_INVALID_ARG, MSD_ERR_CAPACITY, MSD_ERR_STATE, MSD_ERR_HIP = 0, -1, -2, -3, -4
 TREE_STATIC, TREE_DYNAMIC = 0, 1
+F32, BF16, F16 = 0, 1, 2      # float types of the microscaled operators
+MX_ROWS, MX_WEIGHT = 0, 1     # layouts of a quantised matrix
 
 c_i32, c_f32, c_vp, c_sz = ctypes.c_int32, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t
 
@@ -64,6 +66,12 @@ class Tree(ctypes.Structure):
                 ("anc", ctypes.c_uint64 * MAX_TREE)]
 
 
+class Mx(ctypes.Structure):
+    """A quantised matrix (msd_mx)."""
+    _fields_ = [("codes_d", c_vp), ("scales_d", c_vp), ("rows", c_i32), ("cols", c_i32),
+                ("layout", c_i32), ("terms", c_i32)]
+
+
 _lib = None
 
 
@@ -103,6 +111,13 @@ def lib():
         L.msd_train_lr.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.c_double,
                                    P(ctypes.c_double)]
         L.msd_train_mix.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.c_int, P(c_i32), P(c_i32)]
+        L.msd_mx_bytes.argtypes = [P(Mx), P(c_sz), P(c_sz)]
+        L.msd_mx_quantize.argtypes = [c_vp, ctypes.c_int, c_sz, P(Mx), c_vp]
+        L.msd_mx_dequantize.argtypes = [P(Mx), c_vp, ctypes.c_int, c_sz, c_vp]
+        L.msd_mx_resid_norm.argtypes = [c_vp, c_sz, c_vp, c_sz, c_vp, c_sz, ctypes.c_int, c_vp,
+                                        c_f32, P(Mx), c_vp]
+        L.msd_mx_swiglu.argtypes = [c_vp, c_sz, c_vp, c_sz, ctypes.c_int, P(Mx), c_vp]
+        L.msd_mx_product.argtypes = [P(Mx), P(Mx), c_vp, ctypes.c_int, c_sz, c_vp]
         L.msd_trace_enable.argtypes = [c_vp, ctypes.c_int, ctypes.c_int]
         L.msd_trace_read.argtypes = [c_vp, ctypes.c_int, P(TraceRec)]
         _lib = L
@@ -270,6 +285,33 @@ def msd_set_state(ctx, seq, L, h_ptr, next_token):
 
 def msd_stream_read(buf_ptr, nbytes, workgroups, sink_ptr, stream):
     _check(None, lib().msd_stream_read(buf_ptr, nbytes, workgroups, sink_ptr, stream))
+
+
+def msd_mx_bytes(q: Mx):
+    c, s = c_sz(), c_sz()
+    _check(None, lib().msd_mx_bytes(q, ctypes.byref(c), ctypes.byref(s)))
+    return c.value, s.value
+
+
+def msd_mx_quantize(src_ptr, type_, ld, q: Mx, stream):
+    _check(None, lib().msd_mx_quantize(src_ptr, type_, ld, q, stream))
+
+
+def msd_mx_dequantize(q: Mx, dst_ptr, type_, ld, stream):
+    _check(None, lib().msd_mx_dequantize(q, dst_ptr, type_, ld, stream))
+
+
+def msd_mx_resid_norm(x_ptr, ldx, y_ptr, ldy, sum_ptr, lds, type_, gain_ptr, eps, q: Mx, stream):
+    _check(None, lib().msd_mx_resid_norm(x_ptr, ldx, y_ptr, ldy, sum_ptr, lds, type_, gain_ptr,
+                                         eps, q, stream))
+
+
+def msd_mx_swiglu(gate_ptr, ldg, up_ptr, ldu, type_, q: Mx, stream):
+    _check(None, lib().msd_mx_swiglu(gate_ptr, ldg, up_ptr, ldu, type_, q, stream))
+
+
+def msd_mx_product(x: Mx, w: Mx, out_ptr, type_, ld, stream):
+    _check(None, lib().msd_mx_product(x, w, out_ptr, type_, ld, stream))
 
 
 def msd_trace_enable(ctx, capacity, kinds=0xF):
