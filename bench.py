@@ -349,6 +349,8 @@ def main():
                     help="only time plain HBM streaming (read reduction, copy)")
     ap.add_argument("--verify-only", type=int, default=0, metavar="N",
                     help="only run N verify calls on a fixed tree (counter runs)")
+    ap.add_argument("--draft-mx", action="store_true",
+                    help="draft with 4-bit weights (msd_set_draft_mx); default: bfloat16")
     ap.add_argument("--train-step", action="store_true",
                     help="only time the draft training step (accumulate + AdamW apply)")
     ap.add_argument("--late-L", type=int, default=1152,
@@ -399,7 +401,7 @@ def main():
     max_seq = max(max_seq, args.late_L + 64 + T)
     max_seq = (max_seq + 255) // 256 * 256
     eng = B.Engine(dims, w, dr, max_batch=1, max_seq=max_seq, max_tree=64,
-                   max_prompt=wl.prompt_len)
+                   max_prompt=wl.prompt_len, draft_mx=args.draft_mx)
     if wl.tree.kind == "static":
         parent, rank, _ = synth.static_tree_arrays(wl.tree.paths)
         spec = B.make_static_spec(parent[1:], rank[1:])
@@ -525,6 +527,7 @@ def main():
                      if wl.tree.kind == "static" else
                      f"dynamic top-{wl.tree.topk} depth {wl.tree.depth} {wl.tree.n_nodes} nodes"),
             "batch": 1, "draft_fc_init": wl.draft_fc_mode,
+            **({"draft": "4-bit weights"} if args.draft_mx else {}),
         },
         "roofline": {
             "kernel": "msd_verify: the whole verification step (embedding, 32 layers of q/k/v, "

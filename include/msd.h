@@ -213,6 +213,24 @@ int msd_set_draft_input(msd_ctx* ctx, int visual_input);
 int msd_use_caller_weights(msd_ctx* ctx, int enable);
 
 /*
+ * The draft in 4 bits.  With a buffer, the draft phases of the calls that follow
+ * (msd_prefill's draft rows, msd_draft_tree) read the draft's matrices and its LM head
+ * as 4-bit weights and take every product's input in two 4-bit terms (the formats of
+ * msd_mx, below); norms, RoPE, attention, the cache and the residual stay as they are.
+ * The target, and so what is emitted, does not change: a draft's rounding can only
+ * cost acceptance.  The weights are made from the context's packed copies (enqueued on its
+ * stream; nothing is waited for), and again by every msd_train_apply.  NULL: back to the bfloat16
+ * draft.  Sequences may go on across a change (the draft's cache has one format).
+ * msd_trace_enable records no GEMMs of a 4-bit draft.
+ * mx_weights_d: device memory of msd_draft_mx_bytes bytes, 256-byte aligned, valid until
+ * msd_destroy or a call with another buffer.  A draft tree of 26 nodes, 7B-shaped: 0.59 ms (0.88 in bfloat16).
+ * Errors: MSD_ERR_INVALID_ARG (NULL context, misaligned, or d_model or ffn_dim too small
+ * for the workspace to hold the quantised rows: below 40), MSD_ERR_HIP.
+ */
+int msd_draft_mx_bytes(const msd_model_desc* m, size_t* bytes);
+int msd_set_draft_mx(msd_ctx* ctx, void* mx_weights_d);
+
+/*
  * Draft phase for sequences seqs_h[0..n_seq): runs the pending rows through
  * the draft head (text: f_down(Concat(h_i, e_{i+1})); visual: e_i, or h_i
  * after msd_set_draft_input(MSD_DRAFT_VISUAL_FEATURE)), then

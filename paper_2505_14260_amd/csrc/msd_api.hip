@@ -92,6 +92,50 @@ WeightLayout weight_layout(const msd_model_desc& m) {
   return w;
 }
 
+// The draft's weights in 4 bits, in the caller's arena (base null: only sizes):
+// f_down, q|k|v, o, gate|up (up from a row of 16 on), down, the LM head.
+struct DraftMx {
+  MxMat fc, qkv, o, gu, dn, lm;
+  int up;  // gu's first row of up
+  size_t bytes;
+};
+
+DraftMx draft_mx_layout(const msd_model_desc& m, char* base) {
+  const int d = m.d_model, hh = m.n_heads * m.head_dim, F = m.ffn_dim;
+  DraftMx x{};
+  size_t off = 0;
+  const auto take = [&](int rows, int cols) {
+    MxMat q{nullptr, nullptr, rows, cols, 1, true};
+    const size_t codes = off, scales = codes + mx_code_bytes(q);  // multiples of 256
+    off = scales + mx_scale_bytes(q);
+    if (base) q.codes = base + codes, q.scales = base + scales;
+    return q;
+  };
+  x.up = (F + 15) / 16 * 16;
+  x.fc = take(d, 2 * d);
+  x.qkv = take(hh + 2 * m.n_kv_heads * m.head_dim, d);
+  x.o = take(d, hh);
+  x.gu = take(x.up + F, d);
+  x.dn = take(d, F);
+  x.lm = take(m.vocab, d);
+  x.bytes = off;
+  return x;
+}
+
+// Rows [r0, r0 + n) of a quantised matrix (a weight's r0 a multiple of 16).
+MxMat mx_rows(const MxMat& q, int r0, int n) {
+  const MxMat before{nullptr, nullptr, r0, q.cols, q.terms, q.weight};
+  return MxMat{static_cast<char*>(q.codes) + mx_code_bytes(before),
+               static_cast<char*>(q.scales) + mx_scale_bytes(before), n, q.cols, q.terms, q.weight};
+}
+
+// rows of cols activations (two terms) in a workspace buffer of activation rows.
+MxMat mx_act(void* buf, int rows, int cols) {
+  MxMat q{buf, nullptr, rows, cols, 2, false};
+  q.scales = static_cast<char*>(buf) + mx_code_bytes(q);  // rows of 128 bytes and more
+  return q;
+}
+
 constexpr int MSD_MAX_BATCH_ARGS = ATT_MAX_SEQ;
 constexpr int PEND = MSD_MAX_TREE;      // pending draft rows per sequence
 constexpr int FEAT = MSD_MAX_TREE + 1;  // draft feature slots per sequence
@@ -271,6 +315,8 @@ struct msd_ctx {
   int visual_input = MSD_DRAFT_VISUAL_EMBEDDING;  // draft input of visual prompt rows
   TrainState* tr = nullptr;  // draft-head training state (from the first training call)
   bool caller_w = false;     // msd_use_caller_weights
+  bool draft_mx = false;     // msd_set_draft_mx: the draft's weights in 4 bits
+  DraftMx mxw;
   int device;            // the GPU current at msd_create
   float* noalloc_base;   // that GPU's copy of `scratch`
   // host
@@ -680,6 +726,54 @@ struct Wanted {
   const int *list, *out_row;
 };
 
+// The attention of one layer over the queries c->q of n_seq * nq rows, into c->ao:
+// tree attention over a region of tree_R slots, or causal attention of one
+// sequence (tree_R < 0), then of the rows that want names when given; wanted: as
+// launch_causal_attention takes it.
+void launch_attention(msd_ctx* c, uint16_t* kc, uint16_t* vc, int n_seq, int nq, int tree_R,
+                      int max_ltot, const Wanted* want, int wanted) {
+  const msd_model_desc& m = c->m;
+  AttnArgs a{};
+  a.q = c->q;
+  a.kc = kc;
+  a.vc = vc;
+  for (int i = 0; i < n_seq; ++i) {
+    a.seq[i] = c->seq_ids_h[i];
+    a.prefix[i] = c->att_pre[i];
+    a.keys[i] = c->att_keys[i];
+  }
+  a.mask = c->rows.mask;
+  a.S = c->lim.max_seq;
+  a.H = m.n_heads;
+  a.KV = m.n_kv_heads;
+  a.hd = m.head_dim;
+  a.nq = nq;
+  a.n_seq = n_seq;
+  a.out = c->ao;
+  a.scale = 1.0f / std::sqrt((float)m.head_dim);
+  a.part_o = c->att_po;
+  a.part_ml = c->att_ml;
+  a.att_cnt = c->att_cnt;
+  a.place_err = c->att_place;
+  if (tree_R < 0) {
+    a.qtiles = (nq + 31) / 32;
+    a.n_chunks = 1;
+    if (want) {
+      a.row0 = want->row0;
+      a.out_row = want->out_row;
+    }
+    launch_causal_attention(a, wanted, c->st);
+  } else {
+    const TreeChunks tc = plan_tree_chunks(m, n_seq, nq, max_ltot, c->plan.attn_floats);
+    a.qtiles = tc.qtiles;
+    a.chunk_keys = tc.chunk_keys;
+    a.n_chunks = tc.n_chunks;
+    hipEvent_t e0, e1;
+    trace_events(c, TK_ATTN, n_seq * nq, max_ltot, tc.n_chunks, &e0, &e1);
+    launch_tree_attention(a, c->st, e0, e1);
+  }
+}
+
 // One decoder stack (the target's layers or the draft's single layer) over
 // n_seq * nq rows of c->x described by c->rows; c->xn must hold the first
 // layer's input norm.  tree_R < 0 selects causal attention, otherwise tree
@@ -726,55 +820,20 @@ int forward_layers(msd_ctx* c, bool draft, int n_seq, int nq, int tree_R, int ma
                      c->rows.slot + m0, c->rope, c->q + (size_t)m0 * 2 * H * hd, kc, vc, S, c->st);
       LAUNCHED(c);
     }
-    AttnArgs a{};
-    a.q = c->q;
-    a.kc = kc;
-    a.vc = vc;
-    for (int i = 0; i < n_seq; ++i) {
-      a.seq[i] = c->seq_ids_h[i];
-      a.prefix[i] = c->att_pre[i];
-      a.keys[i] = c->att_keys[i];
-    }
-    a.mask = c->rows.mask;
-    a.S = S;
-    a.H = H;
-    a.KV = KV;
-    a.hd = hd;
-    a.nq = nq;
-    a.n_seq = n_seq;
-    a.out = c->ao;
-    a.scale = 1.0f / std::sqrt((float)hd);
-    a.part_o = c->att_po;
-    a.part_ml = c->att_ml;
-    a.att_cnt = c->att_cnt;
-    a.place_err = c->att_place;
-    if (tree_R < 0) {
-      a.qtiles = (nq + 31) / 32;
-      a.n_chunks = 1;
-      if (want && l + 1 == nl) {
-        a.row0 = want->row0;
-        a.out_row = want->out_row;
-        r = want->n;
-        rch = row_chunk(m, r);
-        if (want->list) {
-          x = reinterpret_cast<float*>(c->fcin);  // 4d bf16 a row: free until the draft's pass
-          launch_gather_rows(c->x, want->list, r, d, x, c->st);
-          LAUNCHED(c);
-        } else {
-          x = c->x + (size_t)want->row0 * d;
-        }
+    if (tree_R < 0 && want && l + 1 == nl) {
+      r = want->n;
+      rch = row_chunk(m, r);
+      if (want->list) {
+        x = reinterpret_cast<float*>(c->fcin);  // 4d bf16 a row: free until the draft's pass
+        launch_gather_rows(c->x, want->list, r, d, x, c->st);
+        LAUNCHED(c);
+      } else {
+        x = c->x + (size_t)want->row0 * d;
       }
-      // training: the narrow kernel at every length, for its order of summation
-      launch_causal_attention(a, training ? 0 : r, c->st);
-    } else {
-      const TreeChunks tc = plan_tree_chunks(m, n_seq, nq, max_ltot, c->plan.attn_floats);
-      a.qtiles = tc.qtiles;
-      a.chunk_keys = tc.chunk_keys;
-      a.n_chunks = tc.n_chunks;
-      hipEvent_t e0, e1;
-      trace_events(c, TK_ATTN, rows, max_ltot, tc.n_chunks, &e0, &e1);
-      launch_tree_attention(a, c->st, e0, e1);
     }
+    // training: the narrow kernel at every length, for its order of summation
+    launch_attention(c, kc, vc, n_seq, nq, tree_R, max_ltot, l + 1 == nl ? want : nullptr,
+                     training ? 0 : r);
     LAUNCHED(c);
     for (int m0 = 0; m0 < r; m0 += rch) {
       const int mc = std::min(rch, r - m0);
@@ -813,12 +872,118 @@ int forward_layers(msd_ctx* c, bool draft, int n_seq, int nq, int tree_R, int ma
   return MSD_OK;
 }
 
+// The draft in 4 bits (msd_set_draft_mx): every product's input as two-term rows
+// in a workspace buffer that is free then, float32 results.  The split rows that
+// the other kernels leave are quantised from hi + lo.
+void mx_from_split(msd_ctx* c, const uint16_t* split, const MxMat& q) {
+  launch_mx_quantise(split, MX_SPLIT, 2 * (size_t)q.cols, q, c->st);
+}
+
+// f_down of rows of c->fcin to the float32 rows f.
+int draft_fc_mx(msd_ctx* c, int rows, float* f) {
+  const int d = c->m.d_model;
+  const MxMat in = mx_act(c->xn, rows, 2 * d);
+  mx_from_split(c, c->fcin, in);
+  launch_mx_product(in, c->mxw.fc, f, MX_F32, d, c->st);
+  LAUNCHED(c);
+  return MSD_OK;
+}
+
+// The draft's decoder layer over rows c->x (forward_layers' draft form).
+int draft_layer_mx(msd_ctx* c, int n_seq, int nq, int tree_R, int max_ltot, uint16_t* final_xb,
+                   const int* feat_dst, float* feat, const Wanted* want) {
+  const msd_model_desc& m = c->m;
+  const int rows = n_seq * nq, d = m.d_model, H = m.n_heads, KV = m.n_kv_heads, hd = m.head_dim;
+  const int F = m.ffn_dim;
+  const DraftMx& w = c->mxw;
+  const RowNorm none{nullptr, 0, 0, 0.f};
+  // a product's rows [m0, m0 + mc) of `in` as the consumers of partials take them
+  const auto product = [&](const MxMat& in, int m0, int mc, const MxMat& wt, int off2, Parts* pt) {
+    const int ld = (wt.rows + 3) / 4 * 4;
+    if ((size_t)mc * ld > c->plan.part_floats)
+      return fail(c, MSD_ERR_INVALID_ARG, "internal: product exceeds its buffer");
+    launch_mx_product(mx_rows(in, m0, mc), wt, c->part, MX_F32, ld, c->st);
+    *pt = Parts{c->part, 1, 0, ld, off2};
+    LAUNCHED(c);
+    return (int)MSD_OK;
+  };
+  Parts pt;
+  const int ch = row_chunk(m, rows);
+  const MxMat a1 = mx_act(c->xn, rows, d);
+  launch_mx_norm(c->x, d, nullptr, 0, nullptr, 0, MX_F32, c->dlayer.n1, m.norm_eps, a1, c->st);
+  LAUNCHED(c);
+  for (int m0 = 0; m0 < rows; m0 += ch) {
+    const int mc = std::min(ch, rows - m0);
+    TRY(product(a1, m0, mc, w.qkv, 0, &pt));
+    launch_rope_kv(pt, none, mc, H, KV, hd, c->rows.pos + m0, c->rows.seq + m0, c->rows.slot + m0,
+                   c->rope, c->q + (size_t)m0 * 2 * H * hd, c->dk, c->dv, c->lim.max_seq, c->st);
+    LAUNCHED(c);
+  }
+  const int r = want ? want->n : rows, rch = row_chunk(m, r);
+  float* const x = c->x + (want ? (size_t)want->row0 * d : 0);
+  launch_attention(c, c->dk, c->dv, n_seq, nq, tree_R, max_ltot, want, r);
+  LAUNCHED(c);
+  const MxMat o = mx_act(c->q, r, H * hd);
+  mx_from_split(c, c->ao, o);
+  const MxMat a2 = mx_act(c->xn, r, d), act = mx_act(c->act, r, F);
+  for (int m0 = 0; m0 < r; m0 += rch) {
+    const int mc = std::min(rch, r - m0);
+    float* const xm = x + (size_t)m0 * d;
+    TRY(product(o, m0, mc, w.o, 0, &pt));
+    launch_mx_norm(xm, d, pt.p, pt.ld, xm, d, MX_F32, c->dlayer.n2, m.norm_eps, mx_rows(a2, m0, mc),
+                   c->st);
+    LAUNCHED(c);
+  }
+  for (int m0 = 0; m0 < r; m0 += rch) {
+    const int mc = std::min(rch, r - m0);
+    TRY(product(a2, m0, mc, w.gu, w.up, &pt));
+    launch_mx_swiglu(pt.p, pt.ld, pt.p + pt.off2, pt.ld, MX_F32, mx_rows(act, m0, mc), c->st);
+    LAUNCHED(c);
+  }
+  for (int m0 = 0; m0 < r; m0 += rch) {
+    const int mc = std::min(rch, r - m0);
+    TRY(product(act, m0, mc, w.dn, 0, &pt));
+    launch_resid(pt, mc, d, RN_ADD, x + (size_t)m0 * d, nullptr, nullptr,
+                 final_xb ? final_xb + (size_t)m0 * 2 * d : nullptr, nullptr, c->st,
+                 feat ? feat_dst + m0 : nullptr, feat);
+    LAUNCHED(c);
+  }
+  return MSD_OK;
+}
+
+// (Re)makes the draft's 4-bit weights from the packed bf16 copies; the LM head,
+// which training leaves alone, only when asked.
+int draft_mx_pack(msd_ctx* c, bool lm_head) {
+  const msd_model_desc& m = c->m;
+  const int d = m.d_model, qd = m.n_heads * m.head_dim, kd = m.n_kv_heads * m.head_dim;
+  const size_t pq = packed_elems(qd, d), pk = packed_elems(kd, d);
+  const DraftMx& w = c->mxw;
+  const auto put = [&](const uint16_t* src, const MxMat& q) {
+    launch_mx_quantise(src, MX_PACKED, 0, q, c->st);
+  };
+  put(c->fc_p, w.fc);
+  put(c->pdlayer.qkv, mx_rows(w.qkv, 0, qd));
+  put(c->pdlayer.qkv + pq, mx_rows(w.qkv, qd, kd));
+  put(c->pdlayer.qkv + pq + pk, mx_rows(w.qkv, qd + kd, kd));
+  put(c->pdlayer.o, w.o);
+  put(c->pdlayer.g, mx_rows(w.gu, 0, m.ffn_dim));
+  put(c->pdlayer.u, mx_rows(w.gu, w.up, m.ffn_dim));
+  put(c->pdlayer.d, w.dn);
+  if (lm_head) put(c->lm_p, w.lm);
+  LAUNCHED(c);
+  return MSD_OK;
+}
+
 // Draft head on rows whose f_down input is in c->fcin (split rows of 2d):
 // f = f_down(concat), then the decoder layer; features in c->x and c->xb, and
 // in the feature slots c->rows.dst names (-1: none).
 int draft_pass(msd_ctx* c, int n_seq, int nq, int tree_R, int max_ltot) {
   const int d = c->m.d_model;
   const int rows = n_seq * nq;
+  if (c->draft_mx) {
+    TRY(draft_fc_mx(c, rows, c->x));
+    return draft_layer_mx(c, n_seq, nq, tree_R, max_ltot, c->xb, c->rows.dst, c->dfeat, nullptr);
+  }
   const int ch = row_chunk(c->m, rows);
   Parts pt;
   for (int m0 = 0; m0 < rows; m0 += ch) {
@@ -845,7 +1010,8 @@ int draft_prompt(msd_ctx* c, int n, int n_text, const uint16_t* visual) {
   const bool mixed = n_text != n;
   float* f = mixed ? reinterpret_cast<float*>(c->xb) : c->x;  // xb: 2d bf16 a row
   Parts pt;
-  for (int m0 = 0; m0 < n_text; m0 += ch) {
+  if (c->draft_mx) TRY(draft_fc_mx(c, n_text, f));
+  for (int m0 = 0; m0 < n_text && !c->draft_mx; m0 += ch) {
     const int mc = std::min(ch, n_text - m0);
     TRY(gemm(c, GK_FC, c->fcin + (size_t)m0 * 4 * d, 4 * d, mc, c->fc_p, nullptr, d, 2 * d, &pt));
     launch_resid(pt, mc, d, RN_SET, f + (size_t)m0 * d, mixed ? nullptr : c->dlayer.n1,
@@ -857,9 +1023,11 @@ int draft_prompt(msd_ctx* c, int n, int n_text, const uint16_t* visual) {
     const bool feature = c->visual_input == MSD_DRAFT_VISUAL_FEATURE;
     launch_draft_rows(f, visual, feature ? c->h : nullptr, c->rows.vis, n, d, c->x, c->st);
     LAUNCHED(c);
-    TRY(norm_rows(c, n, c->dlayer.n1));
+    if (!c->draft_mx) TRY(norm_rows(c, n, c->dlayer.n1));
   }
   const Wanted want{1, n - 1, nullptr, nullptr};
+  if (c->draft_mx)
+    return draft_layer_mx(c, 1, n, -1, n, nullptr, c->rows.dst + (n - 1), c->dfeat, &want);
   return forward_layers(c, true, 1, n, -1, n, nullptr, nullptr, nullptr, c->rows.dst + (n - 1),
                         c->dfeat, &want);
 }
@@ -922,9 +1090,17 @@ int prompt_target(msd_ctx* c, int seq, int n, const int32_t* tokens_h,
 int draft_head(msd_ctx* c, int rows, int k) {
   const int d = c->m.d_model, V = c->m.vocab;
   Parts pt;
+  const MxMat in = mx_act(c->xn, rows, d);
+  if (c->draft_mx) mx_from_split(c, c->xb, in);
   for (int m0 = 0; m0 < rows; m0 += LM_ROWS) {
     const int mc = std::min(LM_ROWS, rows - m0);
-    TRY(gemm(c, GK_LMHEAD, c->xb + (size_t)m0 * 2 * d, 2 * d, mc, c->lm_p, nullptr, V, d, &pt));
+    if (c->draft_mx) {
+      pt = Parts{c->part, 1, 0, (V + 3) / 4 * 4, 0};
+      launch_mx_product(mx_rows(in, m0, mc), c->mxw.lm, c->part, MX_F32, pt.ld, c->st);
+      LAUNCHED(c);
+    } else {
+      TRY(gemm(c, GK_LMHEAD, c->xb + (size_t)m0 * 2 * d, 2 * d, mc, c->lm_p, nullptr, V, d, &pt));
+    }
     launch_topk(pt, mc, V, k, c->tk_idx + (size_t)m0 * k, c->tk_val + (size_t)m0 * k,
                 c->tk_lse + m0, c->tk_scratch, c->st);
     LAUNCHED(c);
@@ -1655,6 +1831,38 @@ int msd_use_caller_weights(msd_ctx* c, int enable) {
   return MSD_OK;
 }
 
+int msd_draft_mx_bytes(const msd_model_desc* m, size_t* bytes) {
+  const msd_limits any{1, 8, 1, 1};
+  TRY(check_desc(m, &any, nullptr));
+  if (!bytes) return fail(nullptr, MSD_ERR_INVALID_ARG, "null output pointer");
+  *bytes = draft_mx_layout(*m, nullptr).bytes;
+  return MSD_OK;
+}
+
+int msd_set_draft_mx(msd_ctx* c, void* mx_weights_d) {
+  if (!c) return fail(nullptr, MSD_ERR_INVALID_ARG, "null context");
+  if (!mx_weights_d) {
+    c->draft_mx = false;
+    return MSD_OK;
+  }
+  if ((uintptr_t)mx_weights_d & 255)
+    return fail(c, MSD_ERR_INVALID_ARG, "the 4-bit weights must be 256-byte aligned");
+  const msd_model_desc& m = c->m;
+  // the quantised inputs lie in activation rows of 4d, 4 H hd and 4F bytes
+  const auto fits = [](int cols, int width) {
+    const MxMat q{nullptr, nullptr, 1, cols, 2, false};
+    return mx_code_bytes(q) + mx_scale_bytes(q) <= 4 * (size_t)width;
+  };
+  const int hh = m.n_heads * m.head_dim;
+  if (!fits(2 * m.d_model, m.d_model) || !fits(hh, hh) || !fits(m.ffn_dim, m.ffn_dim))
+    return fail(c, MSD_ERR_INVALID_ARG, "d_model or ffn_dim too small for a draft in 4 bits");
+  c->mxw = draft_mx_layout(m, static_cast<char*>(mx_weights_d));
+  c->draft_mx = false;  // a failure below leaves the draft in bfloat16
+  TRY(draft_mx_pack(c, true));
+  c->draft_mx = true;
+  return MSD_OK;
+}
+
 int msd_set_state(msd_ctx* c, int seq, int L, const void* h_d, int32_t next_token) {
   if (!c) return fail(nullptr, MSD_ERR_INVALID_ARG, "null context");
   if (seq < 0 || seq >= c->lim.max_batch || !h_d) return fail(c, MSD_ERR_INVALID_ARG, "bad argument");
@@ -1991,6 +2199,7 @@ int msd_train_apply(msd_ctx* c, double lr) {
   LAUNCHED(c);
   // with the decoder's packed copies (the norm gains it reads from wb directly)
   TRY(train_pack(c, t, true));
+  if (c->draft_mx) TRY(draft_mx_pack(c, false));
   t->rows = 0;  // the next sequence's gradients replace g
   HIPC(c, hipStreamSynchronize(c->st));
   return MSD_OK;

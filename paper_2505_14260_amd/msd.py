@@ -103,6 +103,8 @@ def lib():
         L.msd_set_state.argtypes = [c_vp, ctypes.c_int, ctypes.c_int, c_vp, c_i32]
         L.msd_set_draft_input.argtypes = [c_vp, ctypes.c_int]
         L.msd_use_caller_weights.argtypes = [c_vp, ctypes.c_int]
+        L.msd_draft_mx_bytes.argtypes = [P(ModelDesc), P(c_sz)]
+        L.msd_set_draft_mx.argtypes = [c_vp, c_vp]
         L.msd_stream_read.argtypes = [c_vp, c_sz, ctypes.c_int, c_vp, c_vp]
         L.msd_train_accumulate.argtypes = [c_vp, ctypes.c_int, ctypes.c_int, P(c_i32),
                                            P(ctypes.c_uint8), c_vp, P(ctypes.c_double)]
@@ -237,6 +239,16 @@ def msd_use_caller_weights(ctx, enable):
     _check(ctx, lib().msd_use_caller_weights(ctx, 1 if enable else 0))
 
 
+def msd_draft_mx_bytes(desc: ModelDesc):
+    n = c_sz()
+    _check(None, lib().msd_draft_mx_bytes(ctypes.byref(desc), ctypes.byref(n)))
+    return n.value
+
+
+def msd_set_draft_mx(ctx, weights_ptr):
+    _check(ctx, lib().msd_set_draft_mx(ctx, weights_ptr))
+
+
 def msd_train_accumulate(ctx, seq, tokens, is_visual, visual_ptr):
     """Loss sums (total, regression, token) of one training sequence; its
     gradient sums are added to the context's."""
@@ -348,7 +360,7 @@ class Engine:
     """Owns device copies of the weights and the caller-side buffers."""
 
     def __init__(self, dims, target, draft, max_batch=1, max_seq=1024, max_tree=64,
-                 max_prompt=1024, device="cuda", visual_input="embedding"):
+                 max_prompt=1024, device="cuda", visual_input="embedding", draft_mx=False):
         import torch
         self.torch = torch
         self.dims = dims
@@ -372,7 +384,10 @@ class Engine:
         self.bufs = Buffers(*[b.data_ptr() for b in self.bufs_t])
         self.stream = torch.cuda.current_stream(self.dev).cuda_stream
         self.ctx = msd_create(self.desc, self.lim, self.tw, self.dw, self.bufs, self.stream)
+        self.draft_mx = None
         self.set_draft_input(visual_input)
+        if draft_mx:
+            self.use_draft_mx()
 
     def set_draft_input(self, visual_input):
         """Draft input of the visual prompt rows of later prefills: "embedding"
@@ -384,6 +399,17 @@ class Engine:
         weights that this engine uploaded (and keeps) instead of unpacking the
         packed copies.  Same results."""
         msd_use_caller_weights(self.ctx, enable)
+
+    def use_draft_mx(self, enable=True):
+        """The draft in 4 bits (msd_set_draft_mx), in a buffer that this engine
+        keeps, or back in bfloat16."""
+        if not enable:
+            msd_set_draft_mx(self.ctx, None)
+            return
+        if self.draft_mx is None:
+            self.draft_mx = self.torch.empty(msd_draft_mx_bytes(self.desc),
+                                             dtype=self.torch.uint8, device=self.dev)
+        msd_set_draft_mx(self.ctx, self.draft_mx.data_ptr())
 
     def train_accumulate(self, seq, tokens, is_visual, visual_bits):
         """Gradient sums of one training sequence; returns its loss sums."""

@@ -138,3 +138,17 @@ def test_tensor_checks():
             call()
     with pytest.raises(msd.MSDError):
         mx.MX(4, 64, layout="weight", terms=2, device="cpu")
+
+
+def test_draft_sizes_and_refusals():
+    d = msd.ModelDesc(2, 128, 4, 2, 64, 300 // 8 * 8, 515, 1e4, 1e-5)
+
+    def weight(n, k):   # 16-row tiles: 4 bits a value of 128 columns, a byte of scale per 32 of 512
+        return -(-n // 16) * 16 * (-(-k // 128) * 64 + -(-k // 512) * 16)
+    F = 296
+    want = (weight(128, 256) + weight(512, 128) + weight(128, 256) + weight(-(-F // 16) * 16 + F, 128)
+            + weight(128, F) + weight(515, 128))
+    assert msd.msd_draft_mx_bytes(d) == want
+    refused(lambda: msd.msd_draft_mx_bytes(msd.ModelDesc(2, 128, 4, 3, 64, 296, 515, 1e4, 1e-5)))
+    refused(lambda: msd.msd_set_draft_mx(None, 0x1000))
+    assert msd.lib().msd_draft_mx_bytes(ctypes.byref(d), None) == msd.MSD_ERR_INVALID_ARG
