@@ -427,8 +427,8 @@ int msd_train_mix(int epoch, int n_epochs, int n_per_epoch, int* n_text_out, int
  * and two scales a value); the matrix stands for the sum.
  *
  * rows (0 .. 2^23) and cols (1 .. 2^20, any), rows * ceil(cols / 512) <= 2^25.
- * layout: MSD_MX_ROWS, row by row (activations; terms 1 or 2), or MSD_MX_WEIGHT, the
- * tiled layout that a product reads its weight in (terms 1).  codes_d and scales_d:
+ * layout: MSD_MX_ROWS (activations; terms 1 or 2) or MSD_MX_WEIGHT (a product's weight;
+ * terms 1).  codes_d and scales_d:
  * 16-byte aligned device buffers of the sizes that msd_mx_bytes gives (it ignores
  * both pointers); their contents are the library's own layout.  No buffer that a
  * call writes may overlap another of its buffers unless the call says so.

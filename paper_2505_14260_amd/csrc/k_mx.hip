@@ -15,16 +15,18 @@
 // cycles of one with an 8-bit operand, and the rounding of two terms is half
 // E4M3's (normal values: 1.5% against 2.9% of their norm; one term 11.5%).
 //
-// Layouts, both in the order in which the product's lanes read a 16 x 128 tile
-// (lane l: row l % 16, block l / 16 of four):
-//  rows    row r: the codes of term 0, of term 1, K padded to 128 columns, two
-//          values a byte, the lower nibble first; its scales, per term groups of
-//          16 blocks (512 columns), block b of a group at byte 4 (b % 4) + b / 4;
-//  weight  tiles (16 rows x 128 columns) of 1 KB, along a row of tiles first, lane
-//          l's 16 bytes at 16 l; the scales of four neighbouring tiles in 256
-//          bytes, lane l's four at 4 l.
-// A lane's dword of scales so serves four tiles.  Padding is zero.
+// Layout: tiles of 16 rows x 128 columns of one term, 1 KB in the order in which the
+// product's lanes read them: lane l's 16 bytes (row l % 16, block l / 16 of four, two
+// values a byte, the lower nibble first) at 16 l.  A row of tiles lies in sequence,
+// per 16 rows first that of term 0, then of term 1.  The scales of four neighbouring
+// tiles (a group, 512 columns) take 256 bytes, lane l's four at 4 l, so that a dword
+// of scales serves four tiles.  Columns past K are zero, scales too; rows past the
+// last are zero in weights and left as they were in activations, whose products are
+// not stored.  Weights (one term) and activations differ in nothing else.
 #include <hip/hip_fp16.h>
+
+#include <algorithm>
+#include <type_traits>
 
 #include "msd_internal.h"
 
@@ -36,6 +38,12 @@ constexpr int BLK = 32;     // values per scale
 constexpr int KT = 128;     // columns of a tile
 constexpr int GROUP = 512;  // columns of a group of scales
 constexpr int TILE_BYTES = 16 * KT / 2;
+
+// Bytes from a row of tiles, and from its scales, to the next: an odd number of tiles
+// and of groups, so that the tiles at one place along K, which all workgroups read
+// at one time, lie in all of an L2's 16 channels (256 bytes each in turn).
+MSD_DEV size_t tiles_pitch(int nkt) { return (size_t)(nkt | 1) * TILE_BYTES; }
+MSD_DEV size_t scales_pitch(int groups) { return (size_t)(groups | 1) * 256; }
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
@@ -155,24 +163,33 @@ MSD_DEV void add_values8(uint32_t codes, uint32_t sc, float* v) {
   }
 }
 
-// Where a lane's eight columns from k0 of a row of the rows layout lie.
+// A quantised matrix of activations to write.
 struct RowsOut {
   uint8_t* codes;
   uint8_t* scales;
-  int term_codes, term_scales;  // bytes of a row per term
-  int terms;
+  int nkt, groups, terms;
 };
 
-MSD_DEV int scale_at(int b) { return (b >> 4) * 16 + (b & 3) * 4 + ((b >> 2) & 3); }
+// Byte offsets of the codes from column k0 on and of the scale of their block.
+MSD_DEV size_t code_at(size_t row, int t, int k0, int terms, int nkt) {
+  const int lane = ((k0 >> 5) & 3) * 16 + (int)(row & 15);
+  return ((row >> 4) * terms + t) * tiles_pitch(nkt) + (k0 >> 7) * TILE_BYTES + lane * 16 +
+         ((k0 & 31) >> 1);
+}
+MSD_DEV size_t scale_at(size_t row, int t, int k0, int terms, int groups) {
+  const int lane = ((k0 >> 5) & 3) * 16 + (int)(row & 15);
+  return ((row >> 4) * terms + t) * scales_pitch(groups) + (k0 >> 9) * 256 + lane * 4 +
+         ((k0 >> 7) & 3);
+}
 
+// Quantises a wave's 512 columns of a row, this lane's eight from k0 on.
 MSD_DEV void put_rows(const RowsOut& o, size_t row, int k0, float* v) {
   for (int t = 0; t < o.terms; ++t) {
     uint32_t sc;
     const uint32_t c = quantise8(v, &sc);
-    if (k0 / 2 < o.term_codes)
-      *reinterpret_cast<uint32_t*>(o.codes + (row * o.terms + t) * o.term_codes + k0 / 2) = c;
-    if (!(threadIdx.x & 3))
-      o.scales[(row * o.terms + t) * o.term_scales + scale_at(k0 / BLK)] = (uint8_t)sc;
+    if (k0 < o.nkt * KT)
+      *reinterpret_cast<uint32_t*>(o.codes + code_at(row, t, k0, o.terms, o.nkt)) = c;
+    if (!(threadIdx.x & 3)) o.scales[scale_at(row, t, k0, o.terms, o.groups)] = (uint8_t)sc;
   }
 }
 
@@ -204,20 +221,22 @@ MSD_DEV void load_src(const Source& s, size_t row, int k0, float* v) {
   }
 }
 
-// Rows layout: a wave takes 512 columns of a row, a lane eight.
+// Activations: a wave takes 512 columns of a row, a lane eight; a workgroup takes 16
+// rows, whose 16-byte pieces of a tile then meet in one L2.
+constexpr int ROW_THREADS = 16 * 64;
 template <int TYPE>
-__global__ __launch_bounds__(256) void k_mx_rows(Source s, int rows, int groups, RowsOut o) {
-  const size_t w = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const size_t row = w / groups;
+__global__ __launch_bounds__(ROW_THREADS) void k_mx_rows(Source s, int rows, RowsOut o) {
+  const size_t tile = blockIdx.x / o.groups;
+  const size_t row = tile * 16 + (threadIdx.x >> 6);
   if (row >= (size_t)rows) return;
-  const int k0 = (int)(w - row * groups) * GROUP + (threadIdx.x & 63) * 8;
+  const int k0 = (int)(blockIdx.x - tile * o.groups) * GROUP + (threadIdx.x & 63) * 8;
   float v[8];
   load_src<TYPE>(s, row, k0, v);
   put_rows(o, row, k0, v);
 }
 
-// Weight layout: a workgroup takes 16 rows of 512 columns, a lane eight columns
-// of a row in each of the four tiles, so that it has its dword of scales.
+// Weights: a workgroup takes 16 rows of 512 columns, a lane eight columns of a row in
+// each of the four tiles, so that it has its dword of scales.
 template <int TYPE>
 __global__ __launch_bounds__(256) void k_mx_weight(Source s, int rows, int groups, int nkt,
                                                    uint8_t* codes, uint32_t* scales) {
@@ -237,14 +256,14 @@ __global__ __launch_bounds__(256) void k_mx_weight(Source s, int rows, int group
     const uint32_t q = quantise8(v, &sc);
     sc4 |= sc << (8 * j);
     if (kt < nkt)
-      *reinterpret_cast<uint32_t*>(codes + (t * nkt + kt) * TILE_BYTES + ((c >> 2) * 16 + r) * 16 +
-                                   (c & 3) * 4) = q;
+      *reinterpret_cast<uint32_t*>(codes + t * tiles_pitch(nkt) + kt * TILE_BYTES +
+                                   ((c >> 2) * 16 + r) * 16 + (c & 3) * 4) = q;
   }
-  if (!(c & 3)) scales[(t * groups + g) * 64 + (c >> 2) * 16 + r] = sc4;
+  if (!(c & 3)) scales[t * (scales_pitch(groups) / 4) + g * 64 + (c >> 2) * 16 + r] = sc4;
 }
 
 // ---------------------------------------------------------- dequantise ----
-template <int TYPE, bool WEIGHT>
+template <int TYPE>
 __global__ __launch_bounds__(256) void k_mx_values(const uint8_t* codes, const uint8_t* scales,
                                                    int terms, int rows, int cols, int units,
                                                    int nkt, int groups, void* out, size_t ld,
@@ -253,22 +272,10 @@ __global__ __launch_bounds__(256) void k_mx_values(const uint8_t* codes, const u
   const size_t row = q / units;
   if (row >= (size_t)rows) return;
   const int k0 = (int)(q - row * units) * 8;
-  const int b = k0 / BLK;
   float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int t = 0; t < terms; ++t) {
-    uint32_t c, sc;
-    if constexpr (WEIGHT) {
-      const size_t tile = row / 16;
-      const int lane = (b & 3) * 16 + (int)(row & 15), kt = k0 / KT;
-      c = *reinterpret_cast<const uint32_t*>(codes + (tile * nkt + kt) * TILE_BYTES + lane * 16 +
-                                             (k0 & 31) / 2);
-      sc = scales[(tile * groups + kt / 4) * 256 + lane * 4 + (kt & 3)];
-    } else {
-      c = *reinterpret_cast<const uint32_t*>(codes + (row * terms + t) * (size_t)(nkt * KT / 2) + k0 / 2);
-      sc = scales[(row * terms + t) * (size_t)(groups * 16) + scale_at(b)];
-    }
-    add_values8(c, sc, v);
-  }
+  for (int t = 0; t < terms; ++t)
+    add_values8(*reinterpret_cast<const uint32_t*>(codes + code_at(row, t, k0, terms, nkt)),
+                scales[scale_at(row, t, k0, terms, groups)], v);
   store8<TYPE>(out, row * ld + k0, cols - k0, vec, v);
 }
 
@@ -277,13 +284,22 @@ __global__ __launch_bounds__(256) void k_mx_values(const uint8_t* codes, const u
 // mean square and the scaling are in float64: 4-bit values change with the last
 // bit of what is rounded to them, and the operator is bound by memory.
 constexpr int NORM_THREADS = 256;
+// From so many rows on, the 16 rows of a tile run on one XCD (workgroup i runs on XCD
+// i mod 8), so that their 16-byte pieces of its codes leave one L2 in whole lines.
+constexpr int NORM_TILE_ROWS = 128;
 template <int TYPE, int CH>
 __global__ __launch_bounds__(NORM_THREADS) void k_mx_norm(const void* x, size_t ldx, const void* y,
                                                           size_t ldy, void* xo, size_t ldo,
-                                                          const uint16_t* gain, int d, double eps,
-                                                          bool vec, bool gvec, RowsOut o) {
+                                                          const uint16_t* gain, int rows, int d,
+                                                          double eps, bool vec, bool gvec,
+                                                          RowsOut o) {
   __shared__ double sh[NORM_THREADS / 64];
-  const size_t row = blockIdx.x;
+  size_t row = blockIdx.x;
+  if (rows >= NORM_TILE_ROWS) {
+    const int i = blockIdx.x >> 3;
+    row = (size_t)((i >> 4) * 8 + (blockIdx.x & 7)) * 16 + (i & 15);
+    if (row >= (size_t)rows) return;
+  }
   float v[CH][8];
   double ss = 0.0;
 #pragma unroll
@@ -310,7 +326,7 @@ __global__ __launch_bounds__(NORM_THREADS) void k_mx_norm(const void* x, size_t 
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const int k0 = (c * NORM_THREADS + (int)threadIdx.x) * 8;
-    if (k0 / 8 / 64 * 64 * 8 >= o.term_scales * BLK) continue;  // a wave past the last group
+    if (k0 / GROUP >= o.groups) continue;  // a wave past the last group
     float g[8];
     load8<MX_BF16>(gain, k0, d - k0, gvec, g);
 #pragma unroll
@@ -321,13 +337,13 @@ __global__ __launch_bounds__(NORM_THREADS) void k_mx_norm(const void* x, size_t 
 
 // -------------------------------------------------------------- swiglu ----
 template <int TYPE>
-__global__ __launch_bounds__(256) void k_mx_swiglu(const void* gate, const void* up, size_t ldg,
-                                                   size_t ldu, int rows, int F, int groups,
-                                                   bool vec, RowsOut o) {
-  const size_t w = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const size_t row = w / groups;
+__global__ __launch_bounds__(ROW_THREADS) void k_mx_swiglu(const void* gate, const void* up,
+                                                           size_t ldg, size_t ldu, int rows, int F,
+                                                           bool vec, RowsOut o) {
+  const size_t tile = blockIdx.x / o.groups;
+  const size_t row = tile * 16 + (threadIdx.x >> 6);
   if (row >= (size_t)rows) return;
-  const int k0 = (int)(w - row * groups) * GROUP + (threadIdx.x & 63) * 8;
+  const int k0 = (int)(blockIdx.x - tile * o.groups) * GROUP + (threadIdx.x & 63) * 8;
   float g[8], u[8];
   load8<TYPE>(gate, row * ldg + k0, F - k0, vec, g);
   load8<TYPE>(up, row * ldu + k0, F - k0, vec, u);
@@ -338,8 +354,8 @@ __global__ __launch_bounds__(256) void k_mx_swiglu(const void* gate, const void*
 
 // ------------------------------------------------------------- product ----
 struct ProductArgs {
-  const uint8_t *xc, *xs;  // rows layout
-  const uint8_t *wc, *ws;  // weight layout
+  const uint8_t *xc, *xs;  // activations
+  const uint8_t *wc, *ws;  // weight
   int M, N, nkt, groups;   // 128-column tiles and groups of four along K
   void* out;
   size_t ldo;
@@ -371,80 +387,316 @@ MSD_DEV void store4(const ProductArgs& a, int m, int n, const f32x4& v) {
 }
 
 // acc += a 16 x 128 tile of W (rows) times one of X (columns): lane l gets the
-// products of X row l % 16 and W rows 4 (l / 16) .. + 3.  The scales are the low
-// bytes of ws and xs.
-MSD_DEV f32x4 mfma_mx(i32x4 w, i32x4 x, f32x4 acc, int ws, int xs) {
+// products of X row l % 16 and W rows 4 (l / 16) .. + 3.  The scales are bytes
+// `byte` (known when compiled) of ws and xs.
+MSD_DEV f32x4 mfma_mx(i32x4 w, i32x4 x, f32x4 acc, int ws, int xs, int byte) {
   const i32x8 w8 = __builtin_shufflevector(w, w, 0, 1, 2, 3, -1, -1, -1, -1);
   const i32x8 x8 = __builtin_shufflevector(x, x, 0, 1, 2, 3, -1, -1, -1, -1);
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, x8, acc, 4, 4, 0, ws, 0, xs);
+#define MX_BYTE(B) __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, x8, acc, 4, 4, B, ws, B, xs)
+  switch (byte) {
+    case 0: return MX_BYTE(0);
+    case 1: return MX_BYTE(1);
+    case 2: return MX_BYTE(2);
+    default: return MX_BYTE(3);
+  }
+#undef MX_BYTE
 }
 
-// Few rows: a workgroup takes 16 columns and 16 MT rows, its waves the groups of
-// K in turn; their sums meet in LDS and are added in the order of the waves.
-template <int MT, int TX, int NW, int TYPE>
-__global__ __launch_bounds__(64 * NW) void k_mx_product(ProductArgs a) {
-  __shared__ f32x4 sh[NW][MT][64];
+// Few rows or few columns: a workgroup takes 16 MT rows and 16 CT columns whole, its
+// eight waves the groups of K in turn, straight from memory to registers, a tile
+// ahead, with no barrier on the way.  Their sums meet in LDS: of waves w and w + 4
+// first, then of the four.
+constexpr int SPLIT_WAVES = 8;
+template <int MT, int CT, int TX, int TYPE>
+__global__ __launch_bounds__(64 * SPLIT_WAVES, 2) void k_mx_split(ProductArgs a, int n_ct) {
+  constexpr int NW = SPLIT_WAVES, U = MT * CT;
+  __shared__ f32x4 sh[NW / 2][U][64];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const unsigned tiles = (a.N + 15) / 16;
-  const int m0 = (int)(blockIdx.x / tiles) * 16 * MT;
-  const size_t tile = blockIdx.x % tiles;
-  const int term_c = a.nkt * (KT / 2), term_s = a.groups * 16;
-  const uint8_t* wc = a.wc + tile * a.nkt * TILE_BYTES + lane * 16;
-  const uint8_t* ws = a.ws + tile * a.groups * 256 + lane * 4;
-  const uint8_t *xc[MT], *xs[MT];
+  const int m0 = (int)(blockIdx.x / n_ct) * MT, n0 = (int)(blockIdx.x % n_ct) * CT;  // in tiles
+  const int xlast = (a.M - 1) >> 4, wlast = (a.N - 1) >> 4, nkt = a.nkt, groups = a.groups;
+  // tiles past the last repeat it; their sums are not stored
+  const uint8_t *xc[MT][TX], *xs[MT][TX], *wc[CT], *ws[CT];
 #pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    // rows past the last repeat it; their sums are not stored
-    const size_t row = min(m0 + m * 16 + (lane & 15), a.M - 1);
-    xc[m] = a.xc + row * TX * term_c + (lane >> 4) * 16;
-    xs[m] = a.xs + row * TX * term_s + (lane >> 4) * 4;
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int t = 0; t < TX; ++t) {
+      const size_t u = (size_t)min(m0 + m, xlast) * TX + t;
+      xc[m][t] = a.xc + u * tiles_pitch(nkt);
+      xs[m][t] = a.xs + u * scales_pitch(groups);
+    }
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const size_t u = min(n0 + c, wlast);
+    wc[c] = a.wc + u * tiles_pitch(nkt);
+    ws[c] = a.ws + u * scales_pitch(groups);
   }
-  f32x4 acc[MT];
+  constexpr int D = MT * TX + CT <= 6 ? 4 : 2;  // tiles in registers
+  i32x4 fx[D][MT][TX], fw[D][CT];
+  int sx[MT][TX], sw[CT], sxn[MT][TX], swn[CT];
+  // tile kt along K; those past the last repeat it, with scales of zero
+  const auto load = [&](int i, int kt) {
+    const unsigned at = (unsigned)min(kt, nkt - 1) * TILE_BYTES + lane * 16;
 #pragma unroll
-  for (int m = 0; m < MT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int g = wave; g < a.groups; g += NW) {
-    const int sw = *reinterpret_cast<const int*>(ws + (size_t)g * 256);
-    int sx[MT][TX];
+    for (int c = 0; c < CT; ++c)
+      fw[i][c] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(wc[c] + at));
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int t = 0; t < TX; ++t)
-        sx[m][t] = *reinterpret_cast<const int*>(xs[m] + t * term_s + g * 16);
+      for (int t = 0; t < TX; ++t) fx[i][m][t] = *reinterpret_cast<const i32x4*>(xc[m][t] + at);
+  };
+  const auto load_s = [&](int g) {
+    const unsigned at = (unsigned)min(g, groups - 1) * 256 + lane * 4;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) swn[c] = *reinterpret_cast<const int*>(ws[c] + at);
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int t = 0; t < TX; ++t) sxn[m][t] = *reinterpret_cast<const int*>(xs[m][t] + at);
+  };
+  f32x4 acc[MT][CT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int c = 0; c < CT; ++c) acc[m][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // the four tiles of group g; `more`: the wave has another one
+  const auto group = [&](int g, bool more) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c) sw[c] = swn[c];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int t = 0; t < TX; ++t) sx[m][t] = sxn[m][t];
+    if (more) load_s(g + NW);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int kt = g * 4 + j;
-      if (kt >= a.nkt) break;
-      const i32x4 w = *reinterpret_cast<const i32x4*>(wc + (size_t)kt * TILE_BYTES);
+      // the tile D - 1 further along the wave's
+      if (j + D - 1 < 4) load((j + D - 1) % D, 4 * g + j + D - 1);
+      else if (more) load((j + D - 1) % D, 4 * (g + NW) + j + D - 5);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int t = 0; t < TX; ++t) {
-          const i32x4 x = *reinterpret_cast<const i32x4*>(xc[m] + t * term_c + kt * (KT / 2));
-          acc[m] = mfma_mx(w, x, acc[m], sw >> (8 * j), sx[m][t] >> (8 * j));
-        }
+        for (int t = 0; t < TX; ++t)
+#pragma unroll
+          for (int c = 0; c < CT; ++c)
+            acc[m][c] = mfma_mx(fw[j % D][c], fx[j % D][m][t], acc[m][c], sw[c], sx[m][t], j);
+      __builtin_amdgcn_sched_barrier(0);
     }
+  };
+  if (wave < groups) {
+    load_s(wave);
+#pragma unroll
+    for (int j = 0; j < D - 1; ++j) load(j, wave * 4 + j);
+    int g = wave;
+#pragma unroll 1
+    for (; g + NW < groups; g += NW) group(g, true);
+    group(g, false);
   }
+  if (wave >= NW / 2) {
 #pragma unroll
-  for (int m = 0; m < MT; ++m) sh[wave][m][lane] = acc[m];
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int c = 0; c < CT; ++c) sh[wave - NW / 2][m * CT + c][lane] = acc[m][c];
+  }
   __syncthreads();
-  for (int u = threadIdx.x; u < MT * 64; u += 64 * NW) {
-    const int m = u >> 6, l = u & 63;
-    f32x4 v = sh[0][m][l];
+  if (wave < NW / 2) {
 #pragma unroll
-    for (int w = 1; w < NW; ++w) v += sh[w][m][l];
-    const int row = m0 + m * 16 + (l & 15), n = (int)tile * 16 + (l >> 4) * 4;
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int c = 0; c < CT; ++c) sh[wave][m * CT + c][lane] += acc[m][c];
+  }
+  __syncthreads();
+  for (int q = threadIdx.x; q < U * 64; q += 64 * NW) {
+    const int u = q >> 6, l = q & 63;
+    f32x4 v = sh[0][u][l];
+#pragma unroll
+    for (int w = 1; w < NW / 2; ++w) v += sh[w][u][l];
+    const int row = (m0 + u / CT) * 16 + (l & 15), n = (n0 + u % CT) * 16 + (l >> 4) * 4;
     if (row < a.M && n < a.N) store4<TYPE>(a, row, n, v);
   }
 }
 
-RowsOut rows_out(const MxMat& q) {
-  return {static_cast<uint8_t*>(q.codes), static_cast<uint8_t*>(q.scales), mx_tiles(q.cols) * KT / 2,
-          mx_groups(q.cols) * 16, q.terms};
+constexpr int COLUMN_GROUP = 4;
+constexpr int RSRC_RAW = 0x00020000;       // raw buffer: 32-bit data format, stride 0
+constexpr int PAST = (int)0x80000000u;     // a byte offset past every buffer
+MSD_DEV constexpr int vmcnt_imm(int n) { return 0x0f70 | (n & 15) | ((n >> 4) << 14); }
+
+// Many rows: a workgroup of RW x CW waves takes 16 WM RW rows and 16 WN CW columns, a
+// wave 16 WM x 16 WN of them.  The tiles of X and W go to LDS by buffer loads with the
+// lds bit, in NB buffers, NB - 1 steps (tiles along K) ahead.
+// The buffers are arrays of their own and the loads into them buffer loads: the
+// compiler then knows that reads of one need not wait for loads into another.  One
+// barrier per step: before it every wave waits for its own loads into the next buffer;
+// later loads stay in flight.
+// Raw buffer loads check voffset against the record count less soffset, so soffset
+// stays inside the buffer: row and column tiles past the last and tiles past K
+// (voffset 2^31) read zeros.
+template <int WM, int WN, int RW, int CW, int NB, int OCC, int TX, int TYPE>
+__global__ __launch_bounds__(64 * RW * CW, OCC) void k_mx_tile(ProductArgs a, int n_mt, int n_nt,
+                                                               int gc) {
+  constexpr int NW = RW * CW, BM = 16 * WM * RW, BN = 16 * WN * CW;
+  constexpr int UX = WM * RW * TX, UW = WN * CW;  // 1 KB pieces of X and of W per step
+  constexpr int XLX = UX / NW, XL = XLX + UW / NW;  // of them per wave: of X, all
+  static_assert(UX % NW == 0 && UW % NW == 0, "pieces divide over the waves");
+  static_assert(NB == 2 || NB == 4, "buffers and bytes of scales repeat every four steps");
+  constexpr bool PRE = NB == 4;  // a step's first fragments are read in the step before
+  constexpr int P = (UX + UW) * 64;
+  __shared__ i32x4 sh0[P];
+  __shared__ i32x4 sh1[P];
+  __shared__ i32x4 sh2[NB == 4 ? P : 1];
+  __shared__ i32x4 sh3[NB == 4 ? P : 1];
+  const auto buf = [&](int i) -> i32x4* {
+    return i % NB == 0 ? sh0 : i % NB == 1 ? sh1 : i % NB == 2 ? sh2 : sh3;
+  };
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int items = n_mt * n_nt, per = (items + 7) >> 3;
+  const int t = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
+  if (((int)blockIdx.x >> 3) >= per || t >= items) return;
+  // groups of gc column tiles, columns innermost
+  const int cg = t / (n_mt * gc), tr = t - cg * n_mt * gc, wide = min(gc, n_nt - cg * gc);
+  const int mt = tr / wide, nt = cg * gc + tr - mt * wide, m0 = mt * BM;
+  const int rw = wave / CW, cw = wave % CW;
+  const int nkt = a.nkt, xtile0 = m0 / 16, xtiles = min((a.M + 15) / 16 - xtile0, BM / 16);
+  const int tiles = (a.N + 15) / 16, tile0 = nt * (BN / 16), ntile = min(tiles - tile0, BN / 16);
+  const int tp = (int)tiles_pitch(nkt), sp = (int)scales_pitch(a.groups);
+  const __amdgpu_buffer_rsrc_t rxc = __builtin_amdgcn_make_buffer_rsrc(
+      (void*)(a.xc + (size_t)xtile0 * TX * tp), 0, xtiles * TX * tp, RSRC_RAW);
+  const __amdgpu_buffer_rsrc_t rxs = __builtin_amdgcn_make_buffer_rsrc(
+      (void*)(a.xs + (size_t)xtile0 * TX * sp), 0, xtiles * TX * sp, RSRC_RAW);
+  const __amdgpu_buffer_rsrc_t rwc = __builtin_amdgcn_make_buffer_rsrc(
+      (void*)(a.wc + (size_t)tile0 * tp), 0, ntile * tp, RSRC_RAW);
+  const __amdgpu_buffer_rsrc_t rws = __builtin_amdgcn_make_buffer_rsrc(
+      (void*)(a.ws + (size_t)tile0 * sp), 0, ntile * sp, RSRC_RAW);
+  int wso[WN], xso[WM][TX];
+#pragma unroll
+  for (int j = 0; j < WN; ++j) wso[j] = (cw * WN + j) * sp + lane * 4;
+#pragma unroll
+  for (int m = 0; m < WM; ++m)
+#pragma unroll
+    for (int tt = 0; tt < TX; ++tt) xso[m][tt] = ((rw * WM + m) * TX + tt) * sp + lane * 4;
+  // piece q of the wave (those of X, then those of W) of tile kt along K
+  const auto load1 = [&](i32x4* b, int q, int kt) {
+    const bool isx = q < XLX;
+    const int u = isx ? wave * XLX + q : wave * (XL - XLX) + q - XLX;
+    const int at = u * tp + lane * 16, vo = kt < nkt ? at : PAST;
+    const int so = min(kt, nkt - 1) * TILE_BYTES;
+    i32x4* const to = b + (isx ? u : UX + u) * 64;
+    if (isx)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rxc, (__attribute__((address_space(3))) void*)to, 16, vo, so, 0, 0);
+    else
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rwc, (__attribute__((address_space(3))) void*)to, 16, vo, so, 0, 0);
+  };
+  constexpr int U = WM * TX, PF = U < 4 ? U : 4;  // X fragments of a step; read PF ahead
+  constexpr int S = WN + U;                       // loads of scales per group
+  i32x4 fw[PRE ? 2 : 1][WN], fx[PF];
+  int sw[WN], sx[WM][TX], swn[WN], sxn[WM][TX];
+  f32x4 acc[WM][WN];
+#pragma unroll
+  for (int m = 0; m < WM; ++m)
+#pragma unroll
+    for (int j = 0; j < WN; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // the scales of group g
+  const auto load_s = [&](int g) {
+    const bool in = g < a.groups;
+    const int at = min(g, a.groups - 1) * 256;
+#pragma unroll
+    for (int j = 0; j < WN; ++j)
+      swn[j] = __builtin_amdgcn_raw_buffer_load_b32(rws, in ? wso[j] : PAST, at, 0);
+#pragma unroll
+    for (int m = 0; m < WM; ++m)
+#pragma unroll
+      for (int tt = 0; tt < TX; ++tt)
+        sxn[m][tt] = __builtin_amdgcn_raw_buffer_load_b32(rxs, in ? xso[m][tt] : PAST, at, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  load_s(0);
+#pragma unroll
+  for (int i = 0; i < NB - 1; ++i) {
+#pragma unroll
+    for (int q = 0; q < XL; ++q) load1(buf(i), q, i);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  constexpr int AHEAD = PRE ? NB - 3 : NB - 2;  // steps whose loads may be in flight at a turn
+  const auto turn = [&](bool scales) {
+    if (AHEAD == 0) __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    else if (scales) __builtin_amdgcn_s_waitcnt(vmcnt_imm(AHEAD * XL + S));
+    else __builtin_amdgcn_s_waitcnt(vmcnt_imm(AHEAD * XL));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  turn(false);
+  const int xo = rw * U * 64 + lane, wo = (UX + cw * WN) * 64 + lane;
+  const auto first = [&](const i32x4* b, int i) {
+#pragma unroll
+    for (int u = 0; u < PF; ++u) fx[u] = b[xo + u * 64];
+#pragma unroll
+    for (int j = 0; j < WN; ++j) fw[PRE ? i & 1 : 0][j] = b[wo + j * 64];
+  };
+  if (PRE) first(sh0, 0);
+  // Step i of a group (known when compiled), tile kt along K.
+  const auto step = [&](int i, int kt) {
+    const i32x4 *const b = buf(i), *const bn = buf(i + 1);
+#pragma unroll
+    for (int q = 0; q < XL; ++q) load1(buf(i + NB - 1), q, kt + NB - 1);
+    __builtin_amdgcn_sched_barrier(0);
+    if (!PRE) first(b, i);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int m = u / TX, tt = u % TX;
+#pragma unroll
+      for (int j = 0; j < WN; ++j)
+        acc[m][j] = mfma_mx(fw[PRE ? i & 1 : 0][j], fx[u % PF], acc[m][j], sw[j], sx[m][tt], i);
+      if (u + PF < U) fx[u % PF] = b[xo + (u + PF) * 64];
+      else if (PRE) fx[u % PF] = bn[xo + (u + PF - U) * 64];
+      if (PRE) {
+#pragma unroll
+        for (int j = u * WN / U; j < (u + 1) * WN / U; ++j) fw[(i + 1) & 1][j] = bn[wo + j * 64];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // the scales of the next group were loaded in a group's first step, before X and W
+    turn(i == 0);
+  };
+#pragma unroll 1
+  for (int g = 0; g < a.groups; ++g) {
+#pragma unroll
+    for (int j = 0; j < WN; ++j) sw[j] = swn[j];
+#pragma unroll
+    for (int m = 0; m < WM; ++m)
+#pragma unroll
+      for (int tt = 0; tt < TX; ++tt) sx[m][tt] = sxn[m][tt];
+    load_s(g + 1);
+    step(0, 4 * g);
+    step(1, 4 * g + 1);
+    step(2, 4 * g + 2);
+    step(3, 4 * g + 3);
+  }
+#pragma unroll
+  for (int m = 0; m < WM; ++m) {
+    const int row = m0 + (rw * WM + m) * 16 + (lane & 15);
+    if (row >= a.M) continue;
+#pragma unroll
+    for (int j = 0; j < WN; ++j) {
+      const int n = (tile0 + cw * WN + j) * 16 + (lane >> 4) * 4;
+      if (n < a.N) store4<TYPE>(a, row, n, acc[m][j]);
+    }
+  }
 }
 
-unsigned wave_blocks(int rows, int groups) {
-  return (unsigned)(((size_t)rows * groups + 3) / 4);
+RowsOut rows_out(const MxMat& q) {
+  return {static_cast<uint8_t*>(q.codes), static_cast<uint8_t*>(q.scales), mx_tiles(q.cols),
+          mx_groups(q.cols), q.terms};
+}
+
+// Workgroups of 16 rows x 512 columns.
+unsigned tile_blocks(const MxMat& q) {
+  return (unsigned)((size_t)((q.rows + 15) / 16) * mx_groups(q.cols));
 }
 
 // Whether rows of values of `size` bytes take 16-byte accesses.
@@ -470,9 +722,8 @@ void launch_mx_quantise(const void* src, int type, size_t ld, const MxMat& q, hi
   s.vec = rows_aligned(src, ld, type == MX_F32 ? 4 : 2);
   if (type == MX_SPLIT) s.vec = s.vec && q.cols % 8 == 0;
   if (q.weight) {
-    const unsigned grid = (unsigned)((size_t)((q.rows + 15) / 16) * groups);
     const auto go = [&](auto k) {
-      hipLaunchKernelGGL(k, dim3(grid), dim3(256), 0, st, s, q.rows, groups, mx_tiles(q.cols),
+      hipLaunchKernelGGL(k, dim3(tile_blocks(q)), dim3(256), 0, st, s, q.rows, groups, mx_tiles(q.cols),
                          static_cast<uint8_t*>(q.codes), static_cast<uint32_t*>(q.scales));
     };
     if (type == MX_PACKED) go(k_mx_weight<MX_PACKED>);
@@ -481,8 +732,7 @@ void launch_mx_quantise(const void* src, int type, size_t ld, const MxMat& q, hi
     else go(k_mx_weight<MX_F16>);
   } else {
     const auto go = [&](auto k) {
-      hipLaunchKernelGGL(k, dim3(wave_blocks(q.rows, groups)), dim3(256), 0, st, s, q.rows, groups,
-                         rows_out(q));
+      hipLaunchKernelGGL(k, dim3(tile_blocks(q)), dim3(ROW_THREADS), 0, st, s, q.rows, rows_out(q));
     };
     if (type == MX_SPLIT) go(k_mx_rows<MX_SPLIT>);
     else if (type == MX_F32) go(k_mx_rows<MX_F32>);
@@ -496,17 +746,10 @@ void launch_mx_dequantise(const MxMat& q, void* dst, int type, size_t ld, hipStr
   const int units = (q.cols + 7) / 8;
   const dim3 grid((unsigned)(((size_t)q.rows * units + 255) / 256));
   const bool vec = rows_aligned(dst, ld, type_size(type));
-#define GO(T)                                                                                      \
-  do {                                                                                             \
-    if (q.weight)                                                                                  \
-      hipLaunchKernelGGL((k_mx_values<T, true>), grid, dim3(256), 0, st, (const uint8_t*)q.codes,  \
-                         (const uint8_t*)q.scales, 1, q.rows, q.cols, units, mx_tiles(q.cols),     \
-                         mx_groups(q.cols), dst, ld, vec);                                         \
-    else                                                                                           \
-      hipLaunchKernelGGL((k_mx_values<T, false>), grid, dim3(256), 0, st, (const uint8_t*)q.codes, \
-                         (const uint8_t*)q.scales, q.terms, q.rows, q.cols, units,                 \
-                         mx_tiles(q.cols), mx_groups(q.cols), dst, ld, vec);                       \
-  } while (0)
+#define GO(T)                                                                                    \
+  hipLaunchKernelGGL((k_mx_values<T>), grid, dim3(256), 0, st, (const uint8_t*)q.codes,          \
+                     (const uint8_t*)q.scales, q.terms, q.rows, q.cols, units, mx_tiles(q.cols), \
+                     mx_groups(q.cols), dst, ld, vec)
   MX_TYPES(type, GO);
 #undef GO
 }
@@ -520,7 +763,8 @@ void launch_mx_norm(const void* x, size_t ldx, const void* y, size_t ldy, void* 
   const bool gvec = !((uintptr_t)gain & 15);
   const RowsOut o = rows_out(q);
   const auto go = [&](auto k) {
-    hipLaunchKernelGGL(k, dim3(q.rows), dim3(NORM_THREADS), 0, st, x, ldx, y, ldy, xo, ldo, gain, d,
+    hipLaunchKernelGGL(k, dim3(q.rows < NORM_TILE_ROWS ? q.rows : (q.rows + 127) / 128 * 128),
+                       dim3(NORM_THREADS), 0, st, x, ldx, y, ldy, xo, ldo, gain, q.rows, d,
                        (double)eps, vec, gvec, o);
   };
   const int per = NORM_THREADS * 8;
@@ -537,14 +781,91 @@ void launch_mx_norm(const void* x, size_t ldx, const void* y, size_t ldy, void* 
 void launch_mx_swiglu(const void* gate, size_t ldg, const void* up, size_t ldu, int type,
                       const MxMat& q, hipStream_t st) {
   if (q.rows <= 0) return;
-  const int groups = mx_groups(q.cols), sz = type_size(type);
+  const int sz = type_size(type);
   const bool vec = rows_aligned(gate, ldg, sz) && rows_aligned(up, ldu, sz);
 #define GO(T)                                                                                    \
-  hipLaunchKernelGGL((k_mx_swiglu<T>), dim3(wave_blocks(q.rows, groups)), dim3(256), 0, st, gate, \
-                     up, ldg, ldu, q.rows, q.cols, groups, vec, rows_out(q))
+  hipLaunchKernelGGL((k_mx_swiglu<T>), dim3(tile_blocks(q)), dim3(ROW_THREADS), 0, st, gate, up, \
+                     ldg, ldu, q.rows, q.cols, vec, rows_out(q))
   MX_TYPES(type, GO);
 #undef GO
 }
+
+namespace {
+
+// How a product runs: the split kernel over tiles of 16 MT rows x 16 CT columns, or
+// (CT = 0) the tile kernel over BM x BN.
+struct ProductPlan {
+  int MT, CT, BM, BN;
+};
+
+// Picks the kernel with the least estimated time (us), from the workgroups W on 256
+// CUs and the groups g of 512 columns of K:
+//  split  2 + l, or from W > 256 on the longer of that and 2 + W c: l, what a workgroup
+//         takes alone, goes by the rounds of g over its eight waves (less for fewer groups
+//         than waves) and the pieces n that it loads per tile along K; c is its share of
+//         the memory path;
+//  tile   f + rounds of W x 4 g steps of s + the output's writing.
+// On the 208 products that the constants were fitted to (11 weights of 512 x 8192 to
+// 32000 x 4096, 1 to 3136 rows, one and two terms) the choice costs 1.2% over the best
+// kernel on average, 35% at worst (96 x 4608 x 3584: 12.3 us for 9.4); a single choice
+// by rows alone, split up to 64, 128 x 256 above, costs 30% on average.
+ProductPlan plan_product(int M, int N, int g, int terms) {
+  ProductPlan best{};
+  float best_us = 0.f;
+  const auto take = [&](float us, const ProductPlan& p) {
+    if (best_us == 0.f || us < best_us) best_us = us, best = p;
+  };
+  const int MT = M <= 16 ? 1 : M <= 32 ? 2 : 4;
+  for (int CT : {1, 2, 4}) {
+    const float W = (float)((M + 16 * MT - 1) / (16 * MT)) * ((N + 16 * CT - 1) / (16 * CT));
+    const int n = MT * terms + CT;
+    const float rounds = g >= SPLIT_WAVES ? (g + SPLIT_WAVES - 1) / SPLIT_WAVES
+                                          : 0.4f + 0.6f * g / SPLIT_WAVES;
+    const float l = rounds * (0.4f * n + 0.4f * CT - 0.3f) + 0.2f * MT * CT;
+    const float c = 1e-3f * (g * (0.22f * n + 0.5f * CT + 0.11f) + 0.8f * MT * CT);
+    take(2.f + (W <= 256.f ? l : std::max(l, W * c)), {MT, CT, 0, 0});
+  }
+  const struct {
+    int BM, BN;
+    float f, s[2];
+  } tiles[] = {{64, 128, 4.f, {0.198f, 0.267f}},
+               {128, 256, 6.5f, {0.55f, 0.79f}},
+               {256, 256, 9.f, {0.78f, 1.24f}}};
+  for (const auto& t : tiles) {
+    const size_t W = (size_t)((M + t.BM - 1) / t.BM) * ((N + t.BN - 1) / t.BN);
+    take(t.f + (float)((W + 255) / 256) * 4 * g * t.s[terms - 1] + (float)M * N * 0.9e-6f,
+         {0, 0, t.BM, t.BN});
+  }
+  return best;
+}
+
+template <int TX, int TYPE>
+void product(const ProductArgs& a, hipStream_t st) {
+  const ProductPlan p = plan_product(a.M, a.N, a.groups, TX);
+  const int n_mt = p.CT ? 0 : (a.M + p.BM - 1) / p.BM, n_nt = p.CT ? 0 : (a.N + p.BN - 1) / p.BN;
+  const auto tile = [&](auto k, int threads) {
+    hipLaunchKernelGGL(k, dim3(8 * ((n_mt * n_nt + 7) / 8)), dim3(threads), 0, st, a, n_mt, n_nt,
+                       COLUMN_GROUP);
+  };
+  const auto split = [&](auto k) {
+    const int n_ct = (a.N + 16 * p.CT - 1) / (16 * p.CT);
+    hipLaunchKernelGGL(k, dim3((unsigned)n_ct * ((a.M + 16 * p.MT - 1) / (16 * p.MT))),
+                       dim3(64 * SPLIT_WAVES), 0, st, a, n_ct);
+  };
+  if (p.BM == 64) tile(k_mx_tile<2, 4, 2, 2, 4, 2, TX, TYPE>, 256);
+  else if (p.BM == 128) tile(k_mx_tile<4, 8, 2, 2, 2, 2, TX, TYPE>, 256);
+  else if (p.BM == 256) tile(k_mx_tile<4, 8, 4, 2, 2, 2, TX, TYPE>, 512);
+#define GO(M)                                             \
+  else if (p.MT == M) {                                   \
+    if (p.CT == 1) split(k_mx_split<M, 1, TX, TYPE>);     \
+    else if (p.CT == 2) split(k_mx_split<M, 2, TX, TYPE>); \
+    else split(k_mx_split<M, 4, TX, TYPE>);               \
+  }
+  GO(1) GO(2) GO(4)
+#undef GO
+}
+
+}  // namespace
 
 void launch_mx_product(const MxMat& x, const MxMat& w, void* out, int type, size_t ldo,
                        hipStream_t st) {
@@ -554,19 +875,10 @@ void launch_mx_product(const MxMat& x, const MxMat& w, void* out, int type, size
                 x.rows, w.rows, mx_tiles(w.cols), mx_groups(w.cols), out, ldo, false};
   const int sz = type_size(type);
   a.vec = !((uintptr_t)out & (4 * sz - 1)) && ldo % 4 == 0;
-  const int MT = x.rows <= 16 ? 1 : 4;
-  const dim3 grid((unsigned)((w.rows + 15) / 16) * ((x.rows + 16 * MT - 1) / (16 * MT)));
-  constexpr int NW = 8;
-  const auto go = [&](auto k) { hipLaunchKernelGGL(k, grid, dim3(64 * NW), 0, st, a); };
-#define GO(T)                                              \
-  do {                                                     \
-    if (x.terms == 2) {                                    \
-      if (MT == 1) go(k_mx_product<1, 2, NW, T>);          \
-      else go(k_mx_product<4, 2, NW, T>);                  \
-    } else {                                               \
-      if (MT == 1) go(k_mx_product<1, 1, NW, T>);          \
-      else go(k_mx_product<4, 1, NW, T>);                  \
-    }                                                      \
+#define GO(T)                               \
+  do {                                      \
+    if (x.terms == 2) product<2, T>(a, st); \
+    else product<1, T>(a, st);              \
   } while (0)
   MX_TYPES(type, GO);
 #undef GO

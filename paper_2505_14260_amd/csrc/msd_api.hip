@@ -122,7 +122,7 @@ DraftMx draft_mx_layout(const msd_model_desc& m, char* base) {
   return x;
 }
 
-// Rows [r0, r0 + n) of a quantised matrix (a weight's r0 a multiple of 16).
+// Rows [r0, r0 + n) of a quantised matrix, r0 a multiple of 16.
 MxMat mx_rows(const MxMat& q, int r0, int n) {
   const MxMat before{nullptr, nullptr, r0, q.cols, q.terms, q.weight};
   return MxMat{static_cast<char*>(q.codes) + mx_code_bytes(before),
@@ -132,7 +132,7 @@ MxMat mx_rows(const MxMat& q, int r0, int n) {
 // rows of cols activations (two terms) in a workspace buffer of activation rows.
 MxMat mx_act(void* buf, int rows, int cols) {
   MxMat q{buf, nullptr, rows, cols, 2, false};
-  q.scales = static_cast<char*>(buf) + mx_code_bytes(q);  // rows of 128 bytes and more
+  q.scales = static_cast<char*>(buf) + mx_code_bytes(q);  // a multiple of 256
   return q;
 }
 
@@ -1848,10 +1848,10 @@ int msd_set_draft_mx(msd_ctx* c, void* mx_weights_d) {
   if ((uintptr_t)mx_weights_d & 255)
     return fail(c, MSD_ERR_INVALID_ARG, "the 4-bit weights must be 256-byte aligned");
   const msd_model_desc& m = c->m;
-  // the quantised inputs lie in activation rows of 4d, 4 H hd and 4F bytes
-  const auto fits = [](int cols, int width) {
-    const MxMat q{nullptr, nullptr, 1, cols, 2, false};
-    return mx_code_bytes(q) + mx_scale_bytes(q) <= 4 * (size_t)width;
+  // the quantised inputs lie in buffers of activation rows of 4d, 4 H hd and 4F bytes
+  const auto fits = [&](int cols, int width) {
+    const MxMat q{nullptr, nullptr, c->plan.rows_max, cols, 2, false};
+    return mx_code_bytes(q) + mx_scale_bytes(q) <= (size_t)c->plan.rows_max * 4 * width;
   };
   const int hh = m.n_heads * m.head_dim;
   if (!fits(2 * m.d_model, m.d_model) || !fits(hh, hh) || !fits(m.ffn_dim, m.ffn_dim))

@@ -406,20 +406,18 @@ struct MxMat {
   void *codes, *scales;
   int rows, cols;
   int terms;    // 1 or 2; a weight has 1
-  bool weight;  // the weight layout, else the rows layout
+  bool weight;  // rows past the last are zero (up to a multiple of 16)
 };
 // Float types of the operators; as sources of a quantisation also a bf16 weight
-// in the packed layout (to the weight layout) and split rows (to the rows layout).
+// in the packed layout (to a weight) and split rows (to activations).
 enum { MX_F32 = 0, MX_BF16 = 1, MX_F16 = 2, MX_PACKED = 3, MX_SPLIT = 4 };
 inline int mx_tiles(int cols) { return (cols + 127) / 128; }
 inline int mx_groups(int cols) { return (cols + 511) / 512; }
 inline size_t mx_code_bytes(const MxMat& q) {
-  const size_t rows = q.weight ? ((size_t)q.rows + 15) / 16 * 16 : (size_t)q.rows;
-  return rows * q.terms * mx_tiles(q.cols) * 64;
+  return ((size_t)q.rows + 15) / 16 * q.terms * (mx_tiles(q.cols) | 1) * 1024;
 }
 inline size_t mx_scale_bytes(const MxMat& q) {
-  const size_t rows = q.weight ? ((size_t)q.rows + 15) / 16 * 16 : (size_t)q.rows;
-  return rows * q.terms * mx_groups(q.cols) * 16;
+  return ((size_t)q.rows + 15) / 16 * q.terms * (mx_groups(q.cols) | 1) * 256;
 }
 void launch_mx_quantise(const void* src, int type, size_t ld, const MxMat& q, hipStream_t st);
 void launch_mx_dequantise(const MxMat& q, void* dst, int type, size_t ld, hipStream_t st);

@@ -92,9 +92,9 @@ def test_product_shapes():
 
 
 def test_overlaps():
-    m = q()   # 2 terms x 64 bytes x 4 rows of codes, 32 bytes x 4 of scales
+    m = q()   # a tile of 1 KB and its scales in 256 bytes, of two terms
     nc, ns = msd.msd_mx_bytes(m)
-    assert (nc, ns) == (512, 128)
+    assert (nc, ns) == (2 * 1024, 2 * 256)
     refused(lambda: msd.msd_mx_quantize(A + nc - 4, msd.F32, 64, m, None))
     refused(lambda: msd.msd_mx_quantize(SRC, msd.F32, 64, q(scales=A + nc - 16), None))
     refused(lambda: msd.msd_mx_dequantize(m, B + ns - 16, msd.F32, 64, None))
@@ -110,11 +110,13 @@ def test_overlaps():
 
 
 @pytest.mark.parametrize("rows, cols, layout, terms, want", [
-    (1, 1, msd.MX_ROWS, 1, (64, 16)), (3, 128, msd.MX_ROWS, 2, (384, 96)),
-    (3, 513, msd.MX_ROWS, 2, (3 * 2 * 5 * 64, 3 * 2 * 2 * 16)),
-    (1, 1, msd.MX_WEIGHT, 1, (1024, 256)), (17, 640, msd.MX_WEIGHT, 1, (32 * 320, 32 * 32)),
-    (0, 64, msd.MX_ROWS, 2, (0, 0)),
-    (152064, 3584, msd.MX_WEIGHT, 1, (152064 * 1792, 152064 * 112))])
+    # tiles of 16 rows x 128 columns, an odd number of them (of four columns of tiles)
+    # along a row
+    (1, 1, msd.MX_ROWS, 1, (1024, 256)), (3, 128, msd.MX_ROWS, 2, (2048, 512)),
+    (17, 513, msd.MX_ROWS, 2, (2 * 2 * 5 * 1024, 2 * 2 * 3 * 256)),
+    (1, 1, msd.MX_WEIGHT, 1, (1024, 256)), (17, 640, msd.MX_WEIGHT, 1, (2 * 5 * 1024, 2 * 3 * 256)),
+    (16, 256, msd.MX_WEIGHT, 1, (3 * 1024, 256)), (0, 64, msd.MX_ROWS, 2, (0, 0)),
+    (152064, 3584, msd.MX_WEIGHT, 1, (9504 * 29 * 1024, 9504 * 7 * 256))])
 def test_sizes(rows, cols, layout, terms, want):
     assert msd.msd_mx_bytes(q(rows, cols, layout, terms)) == want
 
@@ -143,8 +145,8 @@ def test_tensor_checks():
 def test_draft_sizes_and_refusals():
     d = msd.ModelDesc(2, 128, 4, 2, 64, 300 // 8 * 8, 515, 1e4, 1e-5)
 
-    def weight(n, k):   # 16-row tiles: 4 bits a value of 128 columns, a byte of scale per 32 of 512
-        return -(-n // 16) * 16 * (-(-k // 128) * 64 + -(-k // 512) * 16)
+    def weight(n, k):
+        return -(-n // 16) * ((-(-k // 128) | 1) * 1024 + (-(-k // 512) | 1) * 256)
     F = 296
     want = (weight(128, 256) + weight(512, 128) + weight(128, 256) + weight(-(-F // 16) * 16 + F, 128)
             + weight(128, F) + weight(515, 128))
