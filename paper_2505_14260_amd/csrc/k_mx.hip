@@ -48,37 +48,27 @@ MSD_DEV size_t scales_pitch(int groups) { return (size_t)(groups | 1) * 256; }
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// Eight neighbouring values of a float matrix; those at and past n are zero.
+// Sixteen bytes at the alignment of the elements: rows may begin anywhere, and the
+// hardware takes such loads and stores whole (a row of 8,192 odd-aligned bf16 moves
+// at the rate of an aligned one but for the lines that it straddles).
 template <int TYPE>
-MSD_DEV void load8(const void* p, size_t at, int n, bool vec, float* v) {
-  if (vec && n >= 8) {
-    if constexpr (TYPE == MX_F32) {
-      const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
-      const float4 a = q[0], b = q[1];
-      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-      v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    } else {
-      const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + at);
-      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint16_t h = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
-        v[i] = TYPE == MX_BF16 ? bf2f(h) : __half2float(__builtin_bit_cast(__half, h));
-      }
-    }
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    v[i] = 0.f;
-    if (i >= n) continue;
-    if constexpr (TYPE == MX_F32) {
-      v[i] = static_cast<const float*>(p)[at + i];
-    } else {
-      const uint16_t h = static_cast<const uint16_t*>(p)[at + i];
-      v[i] = TYPE == MX_BF16 ? bf2f(h) : __half2float(__builtin_bit_cast(__half, h));
-    }
-  }
+struct Unit;
+template <>
+struct Unit<MX_F32> {
+  typedef uint32_t u32x4_a __attribute__((ext_vector_type(4), aligned(4)));
+  typedef u32x4_a type;
+};
+template <>
+struct Unit<MX_BF16> {
+  typedef uint32_t u32x4_a __attribute__((ext_vector_type(4), aligned(2)));
+  typedef u32x4_a type;
+};
+template <>
+struct Unit<MX_F16> : Unit<MX_BF16> {};
+
+template <int TYPE>
+MSD_DEV float from16(uint16_t h) {
+  return TYPE == MX_BF16 ? bf2f(h) : __half2float(__builtin_bit_cast(__half, h));
 }
 
 template <int TYPE>
@@ -86,19 +76,57 @@ MSD_DEV uint16_t to16(float v) {
   return TYPE == MX_BF16 ? f2bf(v) : __builtin_bit_cast(uint16_t, __float2half(v));
 }
 
+// Eight neighbouring values of a float matrix; those at and past n are zero.
 template <int TYPE>
-MSD_DEV void store8(void* p, size_t at, int n, bool vec, const float* v) {
-  if (vec && n >= 8) {
+MSD_DEV void load8(const void* p, size_t at, int n, float* v) {
+  typedef typename Unit<TYPE>::type U;
+  if (n >= 8) {
     if constexpr (TYPE == MX_F32) {
-      float4* q = reinterpret_cast<float4*>(static_cast<float*>(p) + at);
-      q[0] = make_float4(v[0], v[1], v[2], v[3]);
-      q[1] = make_float4(v[4], v[5], v[6], v[7]);
+      const U* q = reinterpret_cast<const U*>(static_cast<const float*>(p) + at);
+      const U a = q[0], b = q[1];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[i] = __uint_as_float(a[i]);
+        v[4 + i] = __uint_as_float(b[i]);
+      }
     } else {
-      uint32_t w[4];
+      const U a = *reinterpret_cast<const U*>(static_cast<const uint16_t*>(p) + at);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = from16<TYPE>((uint16_t)(a[i / 2] >> (16 * (i & 1))));
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    v[i] = 0.f;
+    if (i >= n) continue;
+    if constexpr (TYPE == MX_F32)
+      v[i] = static_cast<const float*>(p)[at + i];
+    else
+      v[i] = from16<TYPE>(static_cast<const uint16_t*>(p)[at + i]);
+  }
+}
+
+template <int TYPE>
+MSD_DEV void store8(void* p, size_t at, int n, const float* v) {
+  typedef typename Unit<TYPE>::type U;
+  if (n >= 8) {
+    if constexpr (TYPE == MX_F32) {
+      U* q = reinterpret_cast<U*>(static_cast<float*>(p) + at);
+      U a, b;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        a[i] = __float_as_uint(v[i]);
+        b[i] = __float_as_uint(v[4 + i]);
+      }
+      q[0] = a;
+      q[1] = b;
+    } else {
+      U w;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         w[i] = to16<TYPE>(v[2 * i]) | (uint32_t)to16<TYPE>(v[2 * i + 1]) << 16;
-      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+      *reinterpret_cast<U*>(static_cast<uint16_t*>(p) + at) = w;
     }
     return;
   }
@@ -112,9 +140,18 @@ MSD_DEV void store8(void* p, size_t at, int n, bool vec, const float* v) {
   }
 }
 
-// 2^(code - 127), code 0 .. 254
-MSD_DEV float scale_value(uint32_t code) {
-  return __uint_as_float(code ? code << 23 : 0x00400000u);
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// The eight values of a lane's codes under their block's scale (below 255).  The
+// conversion instructions take a scale from the exponent bits alone (0: 2^-127).
+MSD_DEV void values8(uint32_t codes, uint32_t sc, float* v) {
+  const float s = __uint_as_float(sc << 23);
+  const f32x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 0),
+                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 1),
+                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 2),
+                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 3)};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = p[i / 2][i & 1];
 }
 
 // One term of a block whose 32 values lie in four neighbouring lanes, eight
@@ -124,50 +161,37 @@ MSD_DEV uint32_t quantise8(float* v, uint32_t* scale) {
   uint32_t top = 0;  // as bits, so that a NaN is largest
 #pragma unroll
   for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-  const int e = (int)(top >> 23);
-  const bool nan = e == 255;
-  const uint32_t sc = nan ? 255u : (uint32_t)max(e - 2, 0);
-  *scale = sc;
-  const float inv = __uint_as_float((254u - (nan ? 127u : sc)) << 23), s = scale_value(nan ? 127u : sc);
-  uint32_t codes = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float a = fabsf(v[i]) * inv;
-    // the step is 1/2 below 2, 1 below 4, then 2
-    const float step = a < 2.f ? 0.5f : a < 4.f ? 1.f : 2.f;
-    const float per = a < 2.f ? 2.f : a < 4.f ? 1.f : 0.5f;
-    const float q = fminf(__builtin_rintf(a * per) * step, 6.f);
-    // the code of q: 2q up to 2, q + 2 up to 4, q / 2 + 4
-    const uint32_t c = (uint32_t)(q < 2.f ? 2.f * q : q < 4.f ? q + 2.f : 0.5f * q + 4.f);
-    codes |= (c | (__float_as_uint(v[i]) >> 31 << 3)) << (4 * i);
-    v[i] = fmaf(-copysignf(q, v[i]), s, v[i]);
-  }
-  if (nan) {
-    codes = 0;
+  // over four lanes, by moves within quads: lanes 1 0 3 2, then 2 3 0 1
+  top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0xB1, 0xF, 0xF, true));
+  top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x4E, 0xF, 0xF, true));
+  const uint32_t e = top >> 23;
+  if (e == 255u) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(0x7FC00000u);
+    *scale = 255u;
+    return 0u;
   }
+  const uint32_t sc = e > 2u ? e - 2u : 0u;
+  *scale = sc;
+  // the conversions round to the nearest, ties to even, and saturate
+  const float s = __uint_as_float(sc << 23);
+  uint32_t codes = 0;
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, v[0], v[1], s, 0);
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, v[2], v[3], s, 1);
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, v[4], v[5], s, 2);
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, v[6], v[7], s, 3);
+  float q[8];
+  values8(codes, sc, q);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] -= q[i];
   return codes;
 }
 
-// Eight values from their codes and scale, added to v.
-MSD_DEV void add_values8(uint32_t codes, uint32_t sc, float* v) {
-  const float s = sc == 255u ? __uint_as_float(0x7FC00000u) : scale_value(sc);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t c = codes >> (4 * i) & 7u;
-    const float q = c < 4u ? 0.5f * c : c < 6u ? c - 2.f : 2.f * c - 8.f;
-    v[i] += (codes >> (4 * i) & 8u ? -q : q) * s;
-  }
-}
-
-// A quantised matrix of activations to write.
+// A quantised matrix of activations.
 struct RowsOut {
   uint8_t* codes;
   uint8_t* scales;
-  int nkt, groups, terms;
+  int nkt, groups;
 };
 
 // Byte offsets of the codes from column k0 on and of the scale of their block.
@@ -183,13 +207,15 @@ MSD_DEV size_t scale_at(size_t row, int t, int k0, int terms, int groups) {
 }
 
 // Quantises a wave's 512 columns of a row, this lane's eight from k0 on.
+template <int TX>
 MSD_DEV void put_rows(const RowsOut& o, size_t row, int k0, float* v) {
-  for (int t = 0; t < o.terms; ++t) {
+#pragma unroll
+  for (int t = 0; t < TX; ++t) {
     uint32_t sc;
     const uint32_t c = quantise8(v, &sc);
     if (k0 < o.nkt * KT)
-      *reinterpret_cast<uint32_t*>(o.codes + code_at(row, t, k0, o.terms, o.nkt)) = c;
-    if (!(threadIdx.x & 3)) o.scales[scale_at(row, t, k0, o.terms, o.groups)] = (uint8_t)sc;
+      *reinterpret_cast<uint32_t*>(o.codes + code_at(row, t, k0, TX, o.nkt)) = c;
+    if (!(threadIdx.x & 3)) o.scales[scale_at(row, t, k0, TX, o.groups)] = (uint8_t)sc;
   }
 }
 
@@ -200,7 +226,6 @@ struct Source {
   const void* p;
   size_t ld;
   int cols;
-  bool vec;
   int nkt;  // 128-column blocks (packed)
 };
 
@@ -209,22 +234,23 @@ MSD_DEV void load_src(const Source& s, size_t row, int k0, float* v) {
   if constexpr (TYPE == MX_PACKED) {
     const size_t blk = (row >> 6) * s.nkt + (k0 >> 7);
     const size_t unit = (((row >> 4) & 3) * 4 + ((k0 >> 3) & 3)) * 64 + (row & 15) + 16 * ((k0 >> 5) & 3);
-    load8<MX_BF16>(s.p, blk * 8192 + unit * 8, 8, true, v);
+    load8<MX_BF16>(s.p, blk * 8192 + unit * 8, 8, v);
   } else if constexpr (TYPE == MX_SPLIT) {
     float lo[8];
-    load8<MX_BF16>(s.p, row * s.ld + k0, s.cols - k0, s.vec, v);
-    load8<MX_BF16>(s.p, row * s.ld + s.cols + k0, s.cols - k0, s.vec, lo);
+    load8<MX_BF16>(s.p, row * s.ld + k0, s.cols - k0, v);
+    load8<MX_BF16>(s.p, row * s.ld + s.cols + k0, s.cols - k0, lo);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] += lo[i];
   } else {
-    load8<TYPE>(s.p, row * s.ld + k0, s.cols - k0, s.vec, v);
+    load8<TYPE>(s.p, row * s.ld + k0, s.cols - k0, v);
   }
 }
 
-// Activations: a wave takes 512 columns of a row, a lane eight; a workgroup takes 16
-// rows, whose 16-byte pieces of a tile then meet in one L2.
+// Activations: a workgroup takes 16 rows of 512 columns, a wave one of them, a lane
+// eight columns; the rows' 16-byte pieces of a tile so meet in one L2.  (Four rows per
+// wave, their loads together, are slower: 3,136 x 11,008 float32 52 us against 40.)
 constexpr int ROW_THREADS = 16 * 64;
-template <int TYPE>
+template <int TYPE, int TX>
 __global__ __launch_bounds__(ROW_THREADS) void k_mx_rows(Source s, int rows, RowsOut o) {
   const size_t tile = blockIdx.x / o.groups;
   const size_t row = tile * 16 + (threadIdx.x >> 6);
@@ -232,7 +258,7 @@ __global__ __launch_bounds__(ROW_THREADS) void k_mx_rows(Source s, int rows, Row
   const int k0 = (int)(blockIdx.x - tile * o.groups) * GROUP + (threadIdx.x & 63) * 8;
   float v[8];
   load_src<TYPE>(s, row, k0, v);
-  put_rows(o, row, k0, v);
+  put_rows<TX>(o, row, k0, v);
 }
 
 // Weights: a workgroup takes 16 rows of 512 columns, a lane eight columns of a row in
@@ -263,93 +289,108 @@ __global__ __launch_bounds__(256) void k_mx_weight(Source s, int rows, int group
 }
 
 // ---------------------------------------------------------- dequantise ----
-template <int TYPE>
-__global__ __launch_bounds__(256) void k_mx_values(const uint8_t* codes, const uint8_t* scales,
-                                                   int terms, int rows, int cols, int units,
-                                                   int nkt, int groups, void* out, size_t ld,
-                                                   bool vec) {
-  const size_t q = (size_t)blockIdx.x * 256 + threadIdx.x;
-  const size_t row = q / units;
-  if (row >= (size_t)rows) return;
-  const int k0 = (int)(q - row * units) * 8;
-  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int t = 0; t < terms; ++t)
-    add_values8(*reinterpret_cast<const uint32_t*>(codes + code_at(row, t, k0, terms, nkt)),
-                scales[scale_at(row, t, k0, terms, groups)], v);
-  store8<TYPE>(out, row * ld + k0, cols - k0, vec, v);
+// The same workgroups; a wave takes R of the rows.
+template <int TYPE, int TX, int R>
+__global__ __launch_bounds__(ROW_THREADS / R) void k_mx_values(RowsOut q, int rows, int cols,
+                                                               void* out, size_t ld) {
+  const size_t tile = blockIdx.x / q.groups;
+  const size_t row = tile * 16 + (threadIdx.x >> 6) * R;
+  const int k0 = (int)(blockIdx.x - tile * q.groups) * GROUP + (threadIdx.x & 63) * 8;
+  if (k0 >= cols) return;
+  uint32_t c[R][TX], sc[R][TX];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int t = 0; t < TX; ++t) {
+      if (row + i >= (size_t)rows) continue;
+      c[i][t] = *reinterpret_cast<const uint32_t*>(q.codes + code_at(row + i, t, k0, TX, q.nkt));
+      sc[i][t] = q.scales[scale_at(row + i, t, k0, TX, q.groups)];
+    }
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (row + i >= (size_t)rows) continue;
+    float v[8], w[8];
+    values8(c[i][0], sc[i][0], v);
+    if constexpr (TX == 2) {
+      values8(c[i][1], sc[i][1], w);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] += w[k];
+    }
+    if (sc[i][0] == 255u) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(0x7FC00000u);
+    }
+    store8<TYPE>(out, (row + i) * ld + k0, cols - k0, v);
+  }
 }
 
 // ---------------------------------------------------------------- norm ----
 // One workgroup per row, the row's sum in registers between its two uses.  The
 // mean square and the scaling are in float64: 4-bit values change with the last
 // bit of what is rounded to them, and the operator is bound by memory.
-constexpr int NORM_THREADS = 256;
 // From so many rows on, the 16 rows of a tile run on one XCD (workgroup i runs on XCD
 // i mod 8), so that their 16-byte pieces of its codes leave one L2 in whole lines.
 constexpr int NORM_TILE_ROWS = 128;
-template <int TYPE, int CH>
-__global__ __launch_bounds__(NORM_THREADS) void k_mx_norm(const void* x, size_t ldx, const void* y,
-                                                          size_t ldy, void* xo, size_t ldo,
-                                                          const uint16_t* gain, int rows, int d,
-                                                          double eps, bool vec, bool gvec,
-                                                          RowsOut o) {
-  __shared__ double sh[NORM_THREADS / 64];
+template <int TYPE, int NT>
+__global__ __launch_bounds__(NT) void k_mx_norm(const void* x, size_t ldx, const void* y, size_t ldy,
+                                                void* xo, size_t ldo, const uint16_t* gain, int rows,
+                                                int d, double eps, RowsOut o) {
+  __shared__ double sh[NT / 64];
   size_t row = blockIdx.x;
   if (rows >= NORM_TILE_ROWS) {
     const int i = blockIdx.x >> 3;
     row = (size_t)((i >> 4) * 8 + (blockIdx.x & 7)) * 16 + (i & 15);
     if (row >= (size_t)rows) return;
   }
-  float v[CH][8];
+  const int k0 = (int)threadIdx.x * 8, n = d - k0;
+  float v[8], g[8];
+  load8<TYPE>(x, row * ldx + k0, n, v);
+  if (y) {
+    float u[8];
+    load8<TYPE>(y, row * ldy + k0, n, u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += u[i];
+  }
+  load8<MX_BF16>(gain, k0, n, g);
+  if (xo) store8<TYPE>(xo, row * ldo + k0, n, v);
   double ss = 0.0;
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    const int k0 = (c * NORM_THREADS + (int)threadIdx.x) * 8, n = d - k0;
-    load8<TYPE>(x, row * ldx + k0, n, vec, v[c]);
-    if (y) {
-      float u[8];
-      load8<TYPE>(y, row * ldy + k0, n, vec, u);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[c][i] += u[i];
-    }
-    if (xo) store8<TYPE>(xo, row * ldo + k0, n, vec, v[c]);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) ss = fma((double)v[c][i], (double)v[c][i], ss);
-  }
+  for (int i = 0; i < 8; ++i) ss = fma((double)v[i], (double)v[i], ss);
   for (int k = 32; k > 0; k >>= 1) ss += __shfl_xor(ss, k);
   if (!(threadIdx.x & 63)) sh[threadIdx.x >> 6] = ss;
   __syncthreads();
   ss = 0.0;
 #pragma unroll
-  for (int w = 0; w < NORM_THREADS / 64; ++w) ss += sh[w];
+  for (int w = 0; w < NT / 64; ++w) ss += sh[w];
+  if (k0 / GROUP >= o.groups) return;  // a wave past the last group
   const double r = 1.0 / sqrt(ss / d + eps);
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    const int k0 = (c * NORM_THREADS + (int)threadIdx.x) * 8;
-    if (k0 / GROUP >= o.groups) continue;  // a wave past the last group
-    float g[8];
-    load8<MX_BF16>(gain, k0, d - k0, gvec, g);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[c][i] = (float)((double)v[c][i] * r * (double)g[i]);
-    put_rows(o, row, k0, v[c]);
-  }
+  for (int i = 0; i < 8; ++i) v[i] = (float)((double)v[i] * r * (double)g[i]);
+  put_rows<2>(o, row, k0, v);
 }
 
 // -------------------------------------------------------------- swiglu ----
+// g / (1 + e^-g) from t = e^-|g|, which neither overflows nor leaves the reciprocal
+// (1 ulp) a denormal: g r for g >= 0, g t r below, r = 1 / (1 + t).
+MSD_DEV float silu(float g) {
+  const float t = expf(-fabsf(g)), r = __builtin_amdgcn_rcpf(1.f + t);
+  return (g < 0.f ? g * t : g) * r;
+}
+
 template <int TYPE>
 __global__ __launch_bounds__(ROW_THREADS) void k_mx_swiglu(const void* gate, const void* up,
                                                            size_t ldg, size_t ldu, int rows, int F,
-                                                           bool vec, RowsOut o) {
+                                                           RowsOut o) {
   const size_t tile = blockIdx.x / o.groups;
   const size_t row = tile * 16 + (threadIdx.x >> 6);
   if (row >= (size_t)rows) return;
   const int k0 = (int)(blockIdx.x - tile * o.groups) * GROUP + (threadIdx.x & 63) * 8;
   float g[8], u[8];
-  load8<TYPE>(gate, row * ldg + k0, F - k0, vec, g);
-  load8<TYPE>(up, row * ldu + k0, F - k0, vec, u);
+  load8<TYPE>(gate, row * ldg + k0, F - k0, g);
+  load8<TYPE>(up, row * ldu + k0, F - k0, u);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) g[i] = g[i] / (1.f + expf(-g[i])) * u[i];
-  put_rows(o, row, k0, g);
+  for (int i = 0; i < 8; ++i) g[i] = silu(g[i]) * u[i];
+  put_rows<2>(o, row, k0, g);
 }
 
 // ------------------------------------------------------------- product ----
@@ -691,17 +732,12 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void k_mx_tile(ProductArgs a, in
 
 RowsOut rows_out(const MxMat& q) {
   return {static_cast<uint8_t*>(q.codes), static_cast<uint8_t*>(q.scales), mx_tiles(q.cols),
-          mx_groups(q.cols), q.terms};
+          mx_groups(q.cols)};
 }
 
 // Workgroups of 16 rows x 512 columns.
 unsigned tile_blocks(const MxMat& q) {
   return (unsigned)((size_t)((q.rows + 15) / 16) * mx_groups(q.cols));
-}
-
-// Whether rows of values of `size` bytes take 16-byte accesses.
-bool rows_aligned(const void* p, size_t ld, int size) {
-  return !((uintptr_t)p & 15) && !(ld * size & 15);
 }
 
 int type_size(int type) { return type == MX_F32 ? 4 : 2; }
@@ -717,39 +753,47 @@ int type_size(int type) { return type == MX_F32 ? 4 : 2; }
 
 void launch_mx_quantise(const void* src, int type, size_t ld, const MxMat& q, hipStream_t st) {
   if (q.rows <= 0) return;
-  const int groups = mx_groups(q.cols);
-  Source s{src, ld, q.cols, false, mx_tiles(q.cols)};
-  s.vec = rows_aligned(src, ld, type == MX_F32 ? 4 : 2);
-  if (type == MX_SPLIT) s.vec = s.vec && q.cols % 8 == 0;
+  const Source s{src, ld, q.cols, mx_tiles(q.cols)};
   if (q.weight) {
     const auto go = [&](auto k) {
-      hipLaunchKernelGGL(k, dim3(tile_blocks(q)), dim3(256), 0, st, s, q.rows, groups, mx_tiles(q.cols),
-                         static_cast<uint8_t*>(q.codes), static_cast<uint32_t*>(q.scales));
+      hipLaunchKernelGGL(k, dim3(tile_blocks(q)), dim3(256), 0, st, s, q.rows, mx_groups(q.cols),
+                         mx_tiles(q.cols), static_cast<uint8_t*>(q.codes),
+                         static_cast<uint32_t*>(q.scales));
     };
     if (type == MX_PACKED) go(k_mx_weight<MX_PACKED>);
     else if (type == MX_F32) go(k_mx_weight<MX_F32>);
     else if (type == MX_BF16) go(k_mx_weight<MX_BF16>);
     else go(k_mx_weight<MX_F16>);
-  } else {
-    const auto go = [&](auto k) {
-      hipLaunchKernelGGL(k, dim3(tile_blocks(q)), dim3(ROW_THREADS), 0, st, s, q.rows, rows_out(q));
-    };
-    if (type == MX_SPLIT) go(k_mx_rows<MX_SPLIT>);
-    else if (type == MX_F32) go(k_mx_rows<MX_F32>);
-    else if (type == MX_BF16) go(k_mx_rows<MX_BF16>);
-    else go(k_mx_rows<MX_F16>);
+    return;
   }
+  const auto go = [&](auto k) {
+    hipLaunchKernelGGL(k, dim3(tile_blocks(q)), dim3(ROW_THREADS), 0, st, s, q.rows, rows_out(q));
+  };
+#define GO(T)                                 \
+  do {                                        \
+    if (q.terms == 2) go(k_mx_rows<T, 2>);    \
+    else go(k_mx_rows<T, 1>);                 \
+  } while (0)
+  if (type == MX_SPLIT) GO(MX_SPLIT);
+  else MX_TYPES(type, GO);
+#undef GO
 }
 
 void launch_mx_dequantise(const MxMat& q, void* dst, int type, size_t ld, hipStream_t st) {
   if (q.rows <= 0) return;
-  const int units = (q.cols + 7) / 8;
-  const dim3 grid((unsigned)(((size_t)q.rows * units + 255) / 256));
-  const bool vec = rows_aligned(dst, ld, type_size(type));
-#define GO(T)                                                                                    \
-  hipLaunchKernelGGL((k_mx_values<T>), grid, dim3(256), 0, st, (const uint8_t*)q.codes,          \
-                     (const uint8_t*)q.scales, q.terms, q.rows, q.cols, units, mx_tiles(q.cols), \
-                     mx_groups(q.cols), dst, ld, vec)
+  const unsigned blocks = tile_blocks(q);
+  const auto go = [&](auto k, int R) {
+    hipLaunchKernelGGL(k, dim3(blocks), dim3(ROW_THREADS / R), 0, st, rows_out(q), q.rows, q.cols,
+                       dst, ld);
+  };
+  // four rows per wave where one term leaves a wave little to load and there are many
+  // (4,096 x 8,192: 17.5 us against 21.0; with fewer or two terms one row is faster)
+#define GO(T)                                              \
+  do {                                                     \
+    if (q.terms == 2) go(k_mx_values<T, 2, 1>, 1);         \
+    else if (blocks < 2048) go(k_mx_values<T, 1, 1>, 1);   \
+    else go(k_mx_values<T, 1, 4>, 4);                      \
+  } while (0)
   MX_TYPES(type, GO);
 #undef GO
 }
@@ -757,22 +801,17 @@ void launch_mx_dequantise(const MxMat& q, void* dst, int type, size_t ld, hipStr
 void launch_mx_norm(const void* x, size_t ldx, const void* y, size_t ldy, void* xo, size_t ldo,
                     int type, const uint16_t* gain, float eps, const MxMat& q, hipStream_t st) {
   if (q.rows <= 0) return;
-  const int sz = type_size(type), d = q.cols;
-  const bool vec = rows_aligned(x, ldx, sz) && (!y || rows_aligned(y, ldy, sz)) &&
-                   (!xo || rows_aligned(xo, ldo, sz));
-  const bool gvec = !((uintptr_t)gain & 15);
-  const RowsOut o = rows_out(q);
-  const auto go = [&](auto k) {
+  const int d = q.cols;
+  const auto go = [&](auto k, int threads) {
     hipLaunchKernelGGL(k, dim3(q.rows < NORM_TILE_ROWS ? q.rows : (q.rows + 127) / 128 * 128),
-                       dim3(NORM_THREADS), 0, st, x, ldx, y, ldy, xo, ldo, gain, q.rows, d,
-                       (double)eps, vec, gvec, o);
+                       dim3(threads), 0, st, x, ldx, y, ldy, xo, ldo, gain, q.rows, d, (double)eps,
+                       rows_out(q));
   };
-  const int per = NORM_THREADS * 8;
-#define GO(T)                                \
-  do {                                       \
-    if (d <= per) go(k_mx_norm<T, 1>);       \
-    else if (d <= 2 * per) go(k_mx_norm<T, 2>); \
-    else go(k_mx_norm<T, 4>);                \
+#define GO(T)                                          \
+  do {                                                 \
+    if (d <= 2048) go(k_mx_norm<T, 256>, 256);         \
+    else if (d <= 4096) go(k_mx_norm<T, 512>, 512);    \
+    else go(k_mx_norm<T, 1024>, 1024);                 \
   } while (0)
   MX_TYPES(type, GO);
 #undef GO
@@ -781,11 +820,9 @@ void launch_mx_norm(const void* x, size_t ldx, const void* y, size_t ldy, void* 
 void launch_mx_swiglu(const void* gate, size_t ldg, const void* up, size_t ldu, int type,
                       const MxMat& q, hipStream_t st) {
   if (q.rows <= 0) return;
-  const int sz = type_size(type);
-  const bool vec = rows_aligned(gate, ldg, sz) && rows_aligned(up, ldu, sz);
 #define GO(T)                                                                                    \
-  hipLaunchKernelGGL((k_mx_swiglu<T>), dim3(tile_blocks(q)), dim3(ROW_THREADS), 0, st, gate, up, \
-                     ldg, ldu, q.rows, q.cols, vec, rows_out(q))
+  hipLaunchKernelGGL(k_mx_swiglu<T>, dim3(tile_blocks(q)), dim3(ROW_THREADS), 0, st, gate, up, ldg, \
+                     ldu, q.rows, q.cols, rows_out(q))
   MX_TYPES(type, GO);
 #undef GO
 }

@@ -41,20 +41,24 @@ def _float(t, shape, device, what):
         raise ValueError(f"{what}: on {t.device}, the quantised matrix is on {device}")
     if t.dtype not in TYPES:
         raise ValueError(f"{what}: {t.dtype} is not one of float32, bfloat16, float16")
-    rows, cols = shape
     ld, step = t.stride()
-    if cols > 1 and step != 1:
+    if step != 1 and shape[1] > 1:
         raise ValueError(f"{what}: the values of a row must be contiguous")
-    return t.data_ptr(), ld if rows > 1 else max(ld, cols)
+    return t.data_ptr(), ld if shape[0] > 1 else max(ld, shape[1])
+
+
+# the current stream's handle without a Stream object (1.8 us of a call's 6.8)
+_raw_stream = torch._C._cuda_getCurrentRawStream if torch.version.hip else None
 
 
 def _run(device, call, *args):
     """call(*args, stream) with the device current."""
-    if device.index == torch.cuda.current_device():
-        call(*args, torch.cuda.current_stream(device).cuda_stream)
+    i = device.index
+    if torch.cuda.current_device() == i:
+        call(*args, _raw_stream(i))
     else:
-        with torch.cuda.device(device):
-            call(*args, torch.cuda.current_stream(device).cuda_stream)
+        with torch.cuda.device(i):
+            call(*args, _raw_stream(i))
 
 
 def quantize(src, out):

@@ -7,8 +7,8 @@ the oracle's own block changes when its input moves by the operator's error, DEL
 (relative), either way.
   norm: the sum of x and y is the same float32 sum on both sides; float64, then one
   rounding to float32 (2^-24): 2^-23.
-  swiglu: exp within 2^-23 and the sum 1 + e, the quotient and the product rounded
-  once each (2^-24): 2^-23 + 3 * 2^-24 < 2^-21.
+  swiglu: e^-|g| within 2^-23 and the reciprocal within 2^-23, the sum 1 + e and up to
+  three products rounded once each (2^-24): 2 * 2^-23 + 4 * 2^-24 = 2^-21.
 Products: float32 sums of n = cols * terms products: at most n 2^-24 of the sum of
 |x w| (each sum rounded at no more than that size), plus half a step of the output
 type relative to the value.  Where all products are multiples of a u with the sum of
