@@ -268,6 +268,39 @@ def test_product(gentle, terms):
             assert (np.abs(got - full[:r]) <= bound)[fine].all()
 
 
+@pytest.mark.parametrize("rows, n, k", [
+    (635, 22003, 4100),    # workgroup tiles of 128 x 256
+    (1030, 12289, 4096), (2050, 4100, 11000),
+    (3121, 4090, 11000),   # of 256 x 256
+    (385, 32001, 4096)])
+@pytest.mark.parametrize("terms, type_", [(2, "f32"), (1, "bf16"), (2, "f16")])
+def test_product_of_many_rows(rows, n, k, terms, type_):
+    """The largest workgroup tiles, cut at their last rows and columns (the reference:
+    the oracle's values, multiplied in float64 on the GPU)."""
+    from paper_2505_14260_amd import mx
+    g = gen(rows)
+    x, w = torch.randn(rows, k, generator=g), (torch.randn(n, k, generator=g) * 0.02).bfloat16()
+    qx, qw = matrix(rows, k, "rows", terms), matrix(n, k, "weight", 1)
+    mx.quantize(x.cuda(), qx)
+    mx.quantize(w.cuda(), qw)
+    buf = torch.full((rows + 1, n + 3), -3.0, dtype=TYPES[type_], device="cuda")
+    mx.product(qx, qw, buf[:rows, :n])
+    assert (buf[rows:] == -3).all() and (buf[:, n:] == -3).all()
+    a, b = O.quantised(x.double().numpy(), terms), O.term(w.double().numpy())
+    u = torch.outer(*(torch.from_numpy(last_bit(v)).cuda() for v in (a, b)))
+    a, b = torch.from_numpy(a).cuda(), torch.from_numpy(b).cuda()
+    full, size = a @ b.t().contiguous(), a.abs() @ b.abs().t().contiguous()
+    got = buf[:rows, :n].double()
+    if type_ == "f32":
+        firm = size < 2.0 ** 24 * u
+        assert firm.double().mean() > 0.5 and (got == full)[firm].all()
+    bound = k * terms * 2.0 ** -24 * size * (1 + HALF_STEP[type_]) + HALF_STEP[type_] * full.abs() \
+        + (2.0 ** -25 if type_ == "f16" else 0.0)
+    assert (got - full).abs().le(bound).all()
+    # far inside the bound above: a tile gone wrong moves the result by 2^-8 and more
+    assert float((got - full).norm()) <= (2.0 ** -12 + HALF_STEP[type_]) * float(full.norm())
+
+
 @pytest.mark.parametrize("rows", [3, 40, 130, 300])
 def test_product_with_nan_blocks_and_zeros(rows):
     """A NaN block of x takes its row, one of w its column; the rest is as ever."""
@@ -282,6 +315,39 @@ def test_product_with_nan_blocks_and_zeros(rows):
     ref = O.quantised(x.double().numpy(), 2) @ O.term(w.double().numpy()).T
     assert np.isnan(out[2]).all() and np.isnan(out[:, 33]).all()
     assert same(out, ref)
+
+
+def test_offsets_past_32_bits():
+    """A weight of 8.6e9 values (17 GB of bfloat16, 4.9 GB of codes), its last rows
+    against the oracle, with products of few and of many rows."""
+    from paper_2505_14260_amd import mx
+    rows, cols = 131_073, 65_544
+    w = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+    for r in range(0, rows, 16384):
+        w[r:r + 16384].normal_()
+    q = matrix(rows, cols, "weight", 1)
+    assert q.codes.numel() > 2 ** 32
+    print("case: quantise", flush=True)
+    mx.quantize(w, q)
+    tail = O.term(w[-40:].double().cpu().numpy())
+    print("case: values", flush=True)
+    out = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+    mx.dequantize(q, out)
+    assert same(out[-40:].double().cpu().numpy(), tail)
+    del out, w
+    for m in (3, 300):
+        print(f"case: {m} rows", flush=True)
+        x = torch.randn(m, cols, generator=gen(m))
+        qx = matrix(m, cols)
+        mx.quantize(x.cuda(), qx)
+        y = torch.empty(m, rows, device="cuda")
+        mx.product(qx, q, y)
+        v = O.quantised(x.double().numpy(), 2)
+        full, size = v @ tail.T, np.abs(v) @ np.abs(tail).T
+        got = y[:, -40:].double().cpu().numpy()
+        assert (np.abs(got - full) <= 2 * cols * 2.0 ** -24 * size).all()
+        # a relative error of 2^-10 of the sums' own size would be a tile gone wrong
+        assert np.linalg.norm(got - full) <= 2.0 ** -10 * np.linalg.norm(full)
 
 
 def test_empty_matrices():
