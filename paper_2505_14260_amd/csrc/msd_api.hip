@@ -889,9 +889,10 @@ int draft_fc_mx(msd_ctx* c, int rows, float* f) {
   return MSD_OK;
 }
 
-// The draft's decoder layer over rows c->x (forward_layers' draft form).
-int draft_layer_mx(msd_ctx* c, int n_seq, int nq, int tree_R, int max_ltot, uint16_t* final_xb,
-                   const int* feat_dst, float* feat, const Wanted* want) {
+// The draft's decoder layer over rows c->x (forward_layers' draft form).  The features
+// go to their slots and, quantised for the LM head, to c->xn.
+int draft_layer_mx(msd_ctx* c, int n_seq, int nq, int tree_R, int max_ltot, const int* feat_dst,
+                   float* feat, const Wanted* want) {
   const msd_model_desc& m = c->m;
   const int rows = n_seq * nq, d = m.d_model, H = m.n_heads, KV = m.n_kv_heads, hd = m.head_dim;
   const int F = m.ffn_dim;
@@ -942,10 +943,10 @@ int draft_layer_mx(msd_ctx* c, int n_seq, int nq, int tree_R, int max_ltot, uint
   }
   for (int m0 = 0; m0 < r; m0 += rch) {
     const int mc = std::min(rch, r - m0);
+    float* const xm = x + (size_t)m0 * d;
     TRY(product(act, m0, mc, w.dn, 0, &pt));
-    launch_resid(pt, mc, d, RN_ADD, x + (size_t)m0 * d, nullptr, nullptr,
-                 final_xb ? final_xb + (size_t)m0 * 2 * d : nullptr, nullptr, c->st,
-                 feat ? feat_dst + m0 : nullptr, feat);
+    launch_mx_norm(xm, d, pt.p, pt.ld, xm, d, MX_F32, nullptr, 0.f, mx_rows(a2, m0, mc), c->st,
+                   feat_dst + m0, feat);
     LAUNCHED(c);
   }
   return MSD_OK;
@@ -982,7 +983,7 @@ int draft_pass(msd_ctx* c, int n_seq, int nq, int tree_R, int max_ltot) {
   const int rows = n_seq * nq;
   if (c->draft_mx) {
     TRY(draft_fc_mx(c, rows, c->x));
-    return draft_layer_mx(c, n_seq, nq, tree_R, max_ltot, c->xb, c->rows.dst, c->dfeat, nullptr);
+    return draft_layer_mx(c, n_seq, nq, tree_R, max_ltot, c->rows.dst, c->dfeat, nullptr);
   }
   const int ch = row_chunk(c->m, rows);
   Parts pt;
@@ -1027,7 +1028,7 @@ int draft_prompt(msd_ctx* c, int n, int n_text, const uint16_t* visual) {
   }
   const Wanted want{1, n - 1, nullptr, nullptr};
   if (c->draft_mx)
-    return draft_layer_mx(c, 1, n, -1, n, nullptr, c->rows.dst + (n - 1), c->dfeat, &want);
+    return draft_layer_mx(c, 1, n, -1, n, c->rows.dst + (n - 1), c->dfeat, &want);
   return forward_layers(c, true, 1, n, -1, n, nullptr, nullptr, nullptr, c->rows.dst + (n - 1),
                         c->dfeat, &want);
 }
@@ -1086,12 +1087,13 @@ int prompt_target(msd_ctx* c, int seq, int n, const int32_t* tokens_h,
                         all || n_text == n ? nullptr : &want, training);
 }
 
-// LM head + top-k (and log-sum-exp) over the rows of c->xb: no final norm.
-int draft_head(msd_ctx* c, int rows, int k) {
+// LM head + top-k (and log-sum-exp) over the rows of c->xb: no final norm.  A 4-bit
+// draft's layer leaves them quantised in c->xn; the root's are quantised here.
+int draft_head(msd_ctx* c, int rows, int k, bool root) {
   const int d = c->m.d_model, V = c->m.vocab;
   Parts pt;
   const MxMat in = mx_act(c->xn, rows, d);
-  if (c->draft_mx) mx_from_split(c, c->xb, in);
+  if (c->draft_mx && root) mx_from_split(c, c->xb, in);
   for (int m0 = 0; m0 < rows; m0 += LM_ROWS) {
     const int mc = std::min(LM_ROWS, rows - m0);
     if (c->draft_mx) {
@@ -1934,7 +1936,7 @@ int msd_draft_tree(msd_ctx* c, int n_seq, const int32_t* seqs_h, const msd_tree_
   launch_root_feat(n_seq, c->seq_ids, c->dfeat, FEAT, d, c->x, c->xb, c->st);
   LAUNCHED(c);
   if (spec->kind == MSD_TREE_STATIC) {
-    TRY(draft_head(c, n_seq, c->round_k[0]));
+    TRY(draft_head(c, n_seq, c->round_k[0], true));
     launch_tree_init_static(trees_d, n_seq, c->seq_ids, c->d_root, c->sp, T, c->st);
     LAUNCHED(c);
     // round dd expands the depth-dd nodes that have children; its kernel
@@ -1950,7 +1952,7 @@ int msd_draft_tree(msd_ctx* c, int n_seq, const int32_t* seqs_h, const msd_tree_
       const int R = c->round_exp_end[dd];
       for (int i = 0; i < n_seq; ++i) c->att_keys[i] = c->L[seqs_h[i]] + R;
       TRY(draft_pass(c, n_seq, nr, R, max_l + R));
-      TRY(draft_head(c, n_seq * nr, c->round_k[dd]));
+      TRY(draft_head(c, n_seq * nr, c->round_k[dd], false));
       prev_n = nr;
       prev_k = c->round_k[dd];
       prev_depth = dd;
@@ -1959,7 +1961,7 @@ int msd_draft_tree(msd_ctx* c, int n_seq, const int32_t* seqs_h, const msd_tree_
     launch_static_assign(trees_d, n_seq, c->sp, T, prev_depth, c->tk_idx, prev_k, prev_n, c->st);
     LAUNCHED(c);
   } else {
-    TRY(draft_head(c, n_seq, K));
+    TRY(draft_head(c, n_seq, K, true));
     launch_dyn_root(c->pool, n_seq, c->tk_idx, c->tk_val, c->tk_lse, K, c->st);
     LAUNCHED(c);
     int n_pool = K, exp_base = K;
@@ -1972,7 +1974,7 @@ int msd_draft_tree(msd_ctx* c, int n_seq, const int32_t* seqs_h, const msd_tree_
       const int R = exp_base;
       for (int i = 0; i < n_seq; ++i) c->att_keys[i] = c->L[seqs_h[i]] + R;
       TRY(draft_pass(c, n_seq, K, R, max_l + R));
-      TRY(draft_head(c, n_seq * K, K));
+      TRY(draft_head(c, n_seq * K, K, false));
       launch_dyn_expand(c->pool, n_seq, c->tk_idx, c->tk_val, c->tk_lse, K, n_pool, exp_base, c->st);
       LAUNCHED(c);
       n_pool += K * K;

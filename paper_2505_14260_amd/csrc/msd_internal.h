@@ -421,9 +421,12 @@ inline size_t mx_scale_bytes(const MxMat& q) {
 }
 void launch_mx_quantise(const void* src, int type, size_t ld, const MxMat& q, hipStream_t st);
 void launch_mx_dequantise(const MxMat& q, void* dst, int type, size_t ld, hipStream_t st);
-// xo = x + y (when given), q = rmsnorm(x + y) * gain; y and xo may be null
+// xo = x + y (when given), q = rmsnorm(x + y) * gain; y and xo may be null.  gain null:
+// q = x + y, which also goes to row dst[row] of feat (rows of q.cols; dst[row] < 0: not)
+// when feat is given
 void launch_mx_norm(const void* x, size_t ldx, const void* y, size_t ldy, void* xo, size_t ldo,
-                    int type, const uint16_t* gain, float eps, const MxMat& q, hipStream_t st);
+                    int type, const uint16_t* gain, float eps, const MxMat& q, hipStream_t st,
+                    const int* dst = nullptr, float* feat = nullptr);
 // q = silu(gate) * up
 void launch_mx_swiglu(const void* gate, size_t ldg, const void* up, size_t ldu, int type,
                       const MxMat& q, hipStream_t st);
