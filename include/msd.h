@@ -223,9 +223,10 @@ int msd_use_caller_weights(msd_ctx* ctx, int enable);
  * draft.  Sequences may go on across a change (the draft's cache has one format).
  * msd_trace_enable records no GEMMs of a 4-bit draft.
  * mx_weights_d: device memory of msd_draft_mx_bytes bytes, 256-byte aligned, valid until
- * msd_destroy or a call with another buffer.  A draft tree of 26 nodes, 7B-shaped: 0.59 ms (0.88 in bfloat16).
- * Errors: MSD_ERR_INVALID_ARG (NULL context, misaligned, or d_model or ffn_dim too small
- * for the workspace to hold the quantised rows: below 40), MSD_ERR_HIP.
+ * msd_destroy or a call with another buffer.  A draft tree of 26 nodes, 7B-shaped:
+ * 0.53 ms (0.86 in bfloat16).
+ * Errors: MSD_ERR_INVALID_ARG (NULL context, misaligned, or d_model, ffn_dim or n_heads *
+ * head_dim too small for the workspace to hold the quantised rows: below 96), MSD_ERR_HIP.
  */
 int msd_draft_mx_bytes(const msd_model_desc* m, size_t* bytes);
 int msd_set_draft_mx(msd_ctx* ctx, void* mx_weights_d);
@@ -431,7 +432,8 @@ int msd_train_mix(int epoch, int n_epochs, int n_per_epoch, int* n_text_out, int
  * terms 1).  codes_d and scales_d:
  * 16-byte aligned device buffers of the sizes that msd_mx_bytes gives (it ignores
  * both pointers); their contents are the library's own layout.  No buffer that a
- * call writes may overlap another of its buffers unless the call says so.
+ * call writes may overlap another of its buffers unless the call says so; a float
+ * matrix reaches from its first value to its last, what lies between its rows included.
  *
  * Float matrices are row-major [rows][cols] of `type`, their rows ld >= cols values
  * apart (any; rows that are multiples of 16 bytes apart from a 16-byte aligned start

@@ -39,18 +39,17 @@ constexpr int KT = 128;     // columns of a tile
 constexpr int GROUP = 512;  // columns of a group of scales
 constexpr int TILE_BYTES = 16 * KT / 2;
 
-// Bytes from a row of tiles, and from its scales, to the next: an odd number of tiles
-// and of groups, so that the tiles at one place along K, which all workgroups read
-// at one time, lie in all of an L2's 16 channels (256 bytes each in turn).
-MSD_DEV size_t tiles_pitch(int nkt) { return (size_t)(nkt | 1) * TILE_BYTES; }
-MSD_DEV size_t scales_pitch(int groups) { return (size_t)(groups | 1) * 256; }
+constexpr int GROUP_SCALES = 256;  // bytes of scales of 16 rows of a group
+
+// Bytes from a row of tiles, and from its scales, to the next.
+MSD_DEV size_t tiles_pitch(int nkt) { return (size_t)nkt * TILE_BYTES; }
+MSD_DEV size_t scales_pitch(int groups) { return (size_t)groups * GROUP_SCALES; }
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 // Sixteen bytes at the alignment of the elements: rows may begin anywhere, and the
-// hardware takes such loads and stores whole (a row of 8,192 odd-aligned bf16 moves
-// at the rate of an aligned one but for the lines that it straddles).
+// hardware takes such loads and stores whole.
 template <int TYPE>
 struct Unit;
 template <>
@@ -202,7 +201,7 @@ MSD_DEV size_t code_at(size_t row, int t, int k0, int terms, int nkt) {
 }
 MSD_DEV size_t scale_at(size_t row, int t, int k0, int terms, int groups) {
   const int lane = ((k0 >> 5) & 3) * 16 + (int)(row & 15);
-  return ((row >> 4) * terms + t) * scales_pitch(groups) + (k0 >> 9) * 256 + lane * 4 +
+  return ((row >> 4) * terms + t) * scales_pitch(groups) + (k0 >> 9) * GROUP_SCALES + lane * 4 +
          ((k0 >> 7) & 3);
 }
 
@@ -249,6 +248,8 @@ MSD_DEV void load_src(const Source& s, size_t row, int k0, float* v) {
 // Activations: a workgroup takes 16 rows of 512 columns, a wave one of them, a lane
 // eight columns; the rows' 16-byte pieces of a tile so meet in one L2.  (Four rows per
 // wave, their loads together, are slower: 3,136 x 11,008 float32 52 us against 40.)
+// Bound by memory once large, by the launch before: 10 x 4,096
+// in 3 us; 3,136 x 11,008 float32 in 40, 175 MB with the codes at 4.4 TB/s of a copy's 4.8.
 constexpr int ROW_THREADS = 16 * 64;
 template <int TYPE, int TX>
 __global__ __launch_bounds__(ROW_THREADS) void k_mx_rows(Source s, int rows, RowsOut o) {
@@ -262,7 +263,8 @@ __global__ __launch_bounds__(ROW_THREADS) void k_mx_rows(Source s, int rows, Row
 }
 
 // Weights: a workgroup takes 16 rows of 512 columns, a lane eight columns of a row in
-// each of the four tiles, so that it has its dword of scales.
+// each of the four tiles, so that it has its dword of scales.  Bound by memory: 4,096 x 8,192
+// bf16, 85 MB, in 20 us (4.2 TB/s).
 template <int TYPE>
 __global__ __launch_bounds__(256) void k_mx_weight(Source s, int rows, int groups, int nkt,
                                                    uint8_t* codes, uint32_t* scales) {
@@ -289,7 +291,8 @@ __global__ __launch_bounds__(256) void k_mx_weight(Source s, int rows, int group
 }
 
 // ---------------------------------------------------------- dequantise ----
-// The same workgroups; a wave takes R of the rows.
+// The same workgroups; a wave takes R of the rows.  Bound by memory: 4,096 x 8,192 of
+// one term to bf16, 85 MB, in 17 us (5.1 TB/s).
 template <int TYPE, int TX, int R>
 __global__ __launch_bounds__(ROW_THREADS / R) void k_mx_values(RowsOut q, int rows, int cols,
                                                                void* out, size_t ld) {
@@ -327,7 +330,8 @@ __global__ __launch_bounds__(ROW_THREADS / R) void k_mx_values(RowsOut q, int ro
 // ---------------------------------------------------------------- norm ----
 // One workgroup per row, the row's sum in registers between its two uses.  The
 // mean square and the scaling are in float64: 4-bit values change with the last
-// bit of what is rounded to them, and the operator is bound by memory.
+// bit of what is rounded to them, and the operator is bound by memory: 3,136 x 4,096
+// float32, 168 MB with the codes, in 37 us (4.5 TB/s); 26 rows of 3,584 bf16 in 4.5, the launch.
 // From so many rows on, the 16 rows of a tile run on one XCD (workgroup i runs on XCD
 // i mod 8), so that their 16-byte pieces of its codes leave one L2 in whole lines.
 constexpr int NORM_TILE_ROWS = 128;
@@ -383,6 +387,8 @@ MSD_DEV float silu(float g) {
   return (g < 0.f ? g * t : g) * r;
 }
 
+// Activations' split (k_mx_rows).  Bound by memory: 640 x 11,008 float32, 64 MB with the
+// codes, in 13.5 us (4.8 TB/s); 10 rows 4.2 us.
 template <int TYPE>
 __global__ __launch_bounds__(ROW_THREADS) void k_mx_swiglu(const void* gate, const void* up,
                                                            size_t ldg, size_t ldu, int rows, int F,
@@ -450,9 +456,11 @@ MSD_DEV f32x4 mfma_mx(i32x4 w, i32x4 x, f32x4 acc, int ws, int xs, int byte) {
 }
 
 // Few rows or few columns: a workgroup takes 16 MT rows and 16 CT columns whole, its
-// eight waves the groups of K in turn, straight from memory to registers, a tile
+// eight waves the groups of K in turn, straight from memory to registers, D - 1 tiles
 // ahead, with no barrier on the way.  Their sums meet in LDS: of waves w and w + 4
-// first, then of the four.
+// first, then of the four.  Eight waves share K so that few columns still fill the
+// chip's memory queues, and each reads 1 KB of W in a row.  Bound by W's bytes: 10 rows by
+// 32,000 x 4,096 (71 MB) in 13 us, 5.5 TB/s; by 4,096 x 4,096 (8.9 MB) in 4.4.
 constexpr int SPLIT_WAVES = 8;
 template <int MT, int CT, int TX, int TYPE>
 __global__ __launch_bounds__(64 * SPLIT_WAVES, 2) void k_mx_split(ProductArgs a, int n_ct) {
@@ -493,7 +501,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES, 2) void k_mx_split(ProductArgs a,
       for (int t = 0; t < TX; ++t) fx[i][m][t] = *reinterpret_cast<const i32x4*>(xc[m][t] + at);
   };
   const auto load_s = [&](int g) {
-    const unsigned at = (unsigned)min(g, groups - 1) * 256 + lane * 4;
+    const unsigned at = (unsigned)min(g, groups - 1) * GROUP_SCALES + lane * 4;
 #pragma unroll
     for (int c = 0; c < CT; ++c) swn[c] = *reinterpret_cast<const int*>(ws[c] + at);
 #pragma unroll
@@ -582,6 +590,11 @@ MSD_DEV constexpr int vmcnt_imm(int n) { return 0x0f70 | (n & 15) | ((n >> 4) <<
 // Raw buffer loads check voffset against the record count less soffset, so soffset
 // stays inside the buffer: row and column tiles past the last and tiles past K
 // (voffset 2^31) read zeros.
+// Bound by feeding the matrix units: 640 x 22,016 x 4,096, two terms, in 59 us, 3.9
+// PFLOP/s of 4-bit products where the same instructions on registers alone reach about 7;
+// its 430 workgroups fill 84% of the places, the units are busy 39% of the time, LDS has
+// no bank conflicts.  W read from memory to registers instead of through LDS is slower
+// (65), a third buffer and K split over two sets of waves are no faster.
 template <int WM, int WN, int RW, int CW, int NB, int OCC, int TX, int TYPE>
 __global__ __launch_bounds__(64 * RW * CW, OCC) void k_mx_tile(ProductArgs a, int n_mt, int n_nt,
                                                                int gc) {
@@ -652,7 +665,7 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void k_mx_tile(ProductArgs a, in
   // the scales of group g
   const auto load_s = [&](int g) {
     const bool in = g < a.groups;
-    const int at = min(g, a.groups - 1) * 256;
+    const int at = min(g, a.groups - 1) * GROUP_SCALES;
 #pragma unroll
     for (int j = 0; j < WN; ++j)
       swn[j] = __builtin_amdgcn_raw_buffer_load_b32(rws, in ? wso[j] : PAST, at, 0);
@@ -853,8 +866,7 @@ struct ProductPlan {
 //  tile   f + rounds of W x 4 g steps of s + the output's writing.
 // On the 208 products that the constants were fitted to (11 weights of 512 x 8192 to
 // 32000 x 4096, 1 to 3136 rows, one and two terms) the choice costs 1.2% over the best
-// kernel on average, 35% at worst (96 x 4608 x 3584: 12.3 us for 9.4); a single choice
-// by rows alone, split up to 64, 128 x 256 above, costs 30% on average.
+// kernel on average, 35% at worst (128 x 4608 x 3584: 13.6 us for 10.1).
 ProductPlan plan_product(int M, int N, int g, int terms) {
   ProductPlan best{};
   float best_us = 0.f;

@@ -976,8 +976,8 @@ int draft_mx_pack(msd_ctx* c, bool lm_head) {
 }
 
 // Draft head on rows whose f_down input is in c->fcin (split rows of 2d):
-// f = f_down(concat), then the decoder layer; features in c->x and c->xb, and
-// in the feature slots c->rows.dst names (-1: none).
+// f = f_down(concat), then the decoder layer; features in c->x, in c->xb (the draft in
+// 4 bits: quantised in c->xn), and in the feature slots c->rows.dst names (-1: none).
 int draft_pass(msd_ctx* c, int n_seq, int nq, int tree_R, int max_ltot) {
   const int d = c->m.d_model;
   const int rows = n_seq * nq;

@@ -414,10 +414,10 @@ enum { MX_F32 = 0, MX_BF16 = 1, MX_F16 = 2, MX_PACKED = 3, MX_SPLIT = 4 };
 inline int mx_tiles(int cols) { return (cols + 127) / 128; }
 inline int mx_groups(int cols) { return (cols + 511) / 512; }
 inline size_t mx_code_bytes(const MxMat& q) {
-  return ((size_t)q.rows + 15) / 16 * q.terms * (mx_tiles(q.cols) | 1) * 1024;
+  return ((size_t)q.rows + 15) / 16 * q.terms * mx_tiles(q.cols) * 1024;
 }
 inline size_t mx_scale_bytes(const MxMat& q) {
-  return ((size_t)q.rows + 15) / 16 * q.terms * (mx_groups(q.cols) | 1) * 256;
+  return ((size_t)q.rows + 15) / 16 * q.terms * mx_groups(q.cols) * 256;
 }
 void launch_mx_quantise(const void* src, int type, size_t ld, const MxMat& q, hipStream_t st);
 void launch_mx_dequantise(const MxMat& q, void* dst, int type, size_t ld, hipStream_t st);

@@ -110,13 +110,12 @@ def test_overlaps():
 
 
 @pytest.mark.parametrize("rows, cols, layout, terms, want", [
-    # tiles of 16 rows x 128 columns, an odd number of them (of four columns of tiles)
-    # along a row
+    # tiles of 16 rows x 128 columns; scales of four columns of tiles together
     (1, 1, msd.MX_ROWS, 1, (1024, 256)), (3, 128, msd.MX_ROWS, 2, (2048, 512)),
-    (17, 513, msd.MX_ROWS, 2, (2 * 2 * 5 * 1024, 2 * 2 * 3 * 256)),
-    (1, 1, msd.MX_WEIGHT, 1, (1024, 256)), (17, 640, msd.MX_WEIGHT, 1, (2 * 5 * 1024, 2 * 3 * 256)),
-    (16, 256, msd.MX_WEIGHT, 1, (3 * 1024, 256)), (0, 64, msd.MX_ROWS, 2, (0, 0)),
-    (152064, 3584, msd.MX_WEIGHT, 1, (9504 * 29 * 1024, 9504 * 7 * 256))])
+    (17, 513, msd.MX_ROWS, 2, (2 * 2 * 5 * 1024, 2 * 2 * 2 * 256)),
+    (1, 1, msd.MX_WEIGHT, 1, (1024, 256)), (17, 640, msd.MX_WEIGHT, 1, (2 * 5 * 1024, 2 * 2 * 256)),
+    (16, 256, msd.MX_WEIGHT, 1, (2 * 1024, 256)), (0, 64, msd.MX_ROWS, 2, (0, 0)),
+    (152064, 3584, msd.MX_WEIGHT, 1, (9504 * 28 * 1024, 9504 * 7 * 256))])
 def test_sizes(rows, cols, layout, terms, want):
     assert msd.msd_mx_bytes(q(rows, cols, layout, terms)) == want
 
@@ -146,7 +145,7 @@ def test_draft_sizes_and_refusals():
     d = msd.ModelDesc(2, 128, 4, 2, 64, 300 // 8 * 8, 515, 1e4, 1e-5)
 
     def weight(n, k):
-        return -(-n // 16) * ((-(-k // 128) | 1) * 1024 + (-(-k // 512) | 1) * 256)
+        return -(-n // 16) * (-(-k // 128) * 1024 + -(-k // 512) * 256)
     F = 296
     want = (weight(128, 256) + weight(512, 128) + weight(128, 256) + weight(-(-F // 16) * 16 + F, 128)
             + weight(128, F) + weight(515, 128))
