@@ -54,6 +54,8 @@ _raw_stream = torch._C._cuda_getCurrentRawStream if torch.version.hip else None
 def _run(device, call, *args):
     """call(*args, stream) with the device current."""
     i = device.index
+    if device.type != "cuda":
+        raise ValueError(f"the matrices must be on a GPU, not on {device}")
     if torch.cuda.current_device() == i:
         call(*args, _raw_stream(i))
     else:

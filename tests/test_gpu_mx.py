@@ -350,6 +350,94 @@ def test_offsets_past_32_bits():
         assert np.linalg.norm(got - full) <= 2.0 ** -10 * np.linalg.norm(full)
 
 
+@pytest.mark.parametrize("rows", [127, 128, 129, 256, 271, 1000])
+def test_norm_of_many_rows(rows):
+    """From 128 rows on they run in another order; a row's result does not depend on
+    how many there are."""
+    from paper_2505_14260_amd import mx
+    x, y = wild(rows, 1100, rows, 3), torch.randn(rows, 1100, generator=gen(9))
+    gain = (1 + 0.2 * torch.randn(1100, generator=gen(8))).bfloat16()
+    xd, yd, gd = x.cuda(), y.cuda(), gain.cuda()
+    out, q = torch.full((rows + 3, 1100), -3.0, device="cuda"), matrix(rows, 1100)
+    mx.resid_norm(xd, yd, gd, 1e-5, out[:rows], q)
+    assert torch.equal(out[:rows].cpu(), x + y) and (out[rows:] == -3).all()
+    v = values(q)
+    near(v, O.rms_norm((x + y).double().numpy(), gain.double().numpy(),
+                       np.float64(np.float32(1e-5))), 2.0 ** -23)
+    for r in range(0, rows, 50):
+        n = min(50, rows - r)
+        part = matrix(n, 1100)
+        mx.resid_norm(xd[r:r + n], yd[r:r + n], gd, 1e-5, None, part)
+        assert same(values(part), v[r:r + n])
+
+
+@pytest.mark.parametrize("layout", ["rows", "weight"])
+@pytest.mark.parametrize("type_", ["f32", "f16"])
+def test_values_of_a_large_matrix(layout, type_):
+    """One term of many rows, whose last are no multiple of four or sixteen."""
+    from paper_2505_14260_amd import mx
+    x = wild(4101, 4100, 3, 3).to(TYPES[type_])
+    q = matrix(4101, 4100, layout, 1)
+    mx.quantize(x.cuda(), q)
+    out = torch.full((4102, 4103), -3.0, dtype=TYPES[type_], device="cuda")
+    mx.dequantize(q, out[:4101, :4100])
+    assert torch.equal(out[:4101, :4100].cpu(), torch.from_numpy(O.term(x.double().numpy())).to(TYPES[type_]))
+    assert (out[4101:] == -3).all() and (out[:, 4100:] == -3).all()
+
+
+def test_most_rows():
+    """2^23 rows of few columns: the operators' largest grids."""
+    from paper_2505_14260_amd import mx
+    rows, cols = 1 << 23, 3
+    x = torch.randn(rows, cols, device="cuda")
+    y = torch.randn(rows, cols, device="cuda")
+    gain = torch.ones(cols, dtype=torch.bfloat16, device="cuda")
+    pick = torch.tensor([0, 1, 15, 16, 127, 128, 1 << 20, 5_000_001, rows - 17, rows - 1])
+    a, b = (t[pick.cuda()].cpu() for t in (x, y))
+    q, out = matrix(rows, cols), torch.empty(rows, cols, device="cuda")
+
+    def got():
+        return mx.dequantize(q, out)[pick.cuda()].double().cpu().numpy()
+    print("case: quantise", flush=True)
+    mx.quantize(x, q)
+    assert same(got(), O.quantised(a.double().numpy(), 2))
+    print("case: norm", flush=True)
+    mx.resid_norm(x, y, gain, 1e-5, None, q)
+    ref = O.rms_norm((a + b).double().numpy(), np.ones(cols), np.float64(np.float32(1e-5)))
+    near(got(), ref, 2.0 ** -23)
+    print("case: swiglu", flush=True)
+    mx.swiglu(x, y, q)
+    near(got(), O.swiglu(a.double().numpy(), b.double().numpy()), 2.0 ** -21)
+    print("case: product", flush=True)
+    w = torch.randn(5, cols, generator=gen(1))
+    qw = mx.quantize(w.cuda(), matrix(5, cols, "weight", 1))
+    mx.quantize(x, q)
+    y = mx.product(q, qw, torch.empty(rows, 5, device="cuda"))[pick.cuda()].double().cpu().numpy()
+    v, u = O.quantised(a.double().numpy(), 2), O.term(w.double().numpy())
+    assert (np.abs(y - v @ u.T) <= 2 * cols * 2.0 ** -24 * (np.abs(v) @ np.abs(u).T)).all()
+
+
+def test_longest_rows():
+    """2^20 columns."""
+    from paper_2505_14260_amd import mx
+    cols = 1 << 20
+    w = torch.randn(33, cols, generator=gen(1)).bfloat16()
+    qw = mx.quantize(w.cuda(), matrix(33, cols, "weight", 1))
+    u = O.term(w.double().numpy())
+    assert same(values(qw), u)
+    for m in (5, 70):
+        print(f"case: {m} rows", flush=True)
+        x = torch.randn(m, cols, generator=gen(m))
+        qx = mx.quantize(x.cuda(), matrix(m, cols))
+        v = O.quantised(x.double().numpy(), 2)
+        assert same(values(qx), v)
+        got = mx.product(qx, qw, torch.empty(m, 33, device="cuda")).double().cpu().numpy()
+        full, size = v @ u.T, np.abs(v) @ np.abs(u).T
+        assert (np.abs(got - full) <= 2 * cols * 2.0 ** -24 * size).all()
+        # a relative error of 2^-10 of the sums' own size would be a tile gone wrong
+        assert np.linalg.norm(got - full) <= 2.0 ** -10 * np.linalg.norm(full)
+
+
 def test_empty_matrices():
     from paper_2505_14260_amd import mx
     q, w = mx.MX(0, 64), mx.MX(16, 64, layout="weight")
@@ -433,6 +521,31 @@ def test_graph_replays_and_streams():
             assert torch.equal(got, eager)
             assert torch.equal(between, ffn(*other))
     torch.cuda.current_stream().wait_stream(stream)
+
+
+def test_two_threads():
+    """Calls of two threads, each on a stream of its own, at one time."""
+    import threading
+    jobs = [ffn_setup(rows, 256, 688, rows)[0] for rows in (20, 300)]
+    want = [ffn(*args).clone() for args in jobs]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(50):
+                    jobs[i][5][4].zero_()
+                    if not torch.equal(ffn(*jobs[i]), want[i]):
+                        wrong.append(i)
+        except Exception as e:   # the thread's failure is the test's
+            wrong.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(60)
+    assert not wrong and not any(t.is_alive() for t in threads)
 
 
 def test_null_stream_entry_points():

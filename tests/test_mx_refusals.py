@@ -134,7 +134,11 @@ def test_tensor_checks():
                  lambda: mx.resid_norm(x, x, g.float(), 1e-5, None, m),
                  lambda: mx.resid_norm(x, x, g[:32], 1e-5, None, m),
                  lambda: mx.swiglu(x, x.half(), m),
-                 lambda: mx.product(m, w, torch.zeros(4, 9))):
+                 lambda: mx.product(m, w, torch.zeros(4, 9)),
+                 # right in all but that they are not on a GPU
+                 lambda: mx.quantize(x, m), lambda: mx.dequantize(m, x),
+                 lambda: mx.resid_norm(x, x, g, 1e-5, None, m), lambda: mx.swiglu(x, x, m),
+                 lambda: mx.product(m, w, torch.zeros(4, 8))):
         with pytest.raises(ValueError):
             call()
     with pytest.raises(msd.MSDError):
