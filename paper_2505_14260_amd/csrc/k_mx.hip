@@ -21,8 +21,9 @@
 // per 16 rows first that of term 0, then of term 1.  The scales of four neighbouring
 // tiles (a group, 512 columns) take 256 bytes, lane l's four at 4 l, so that a dword
 // of scales serves four tiles.  Columns past K are zero, scales too (255 in a row that
-// the norm made all NaN); rows past the last are zero in weights and left as they were in activations, whose products are
-// not stored.  Weights (one term) and activations differ in nothing else.
+// the norm made all NaN); rows past the last are zero in weights and left as they were
+// in activations, whose products are not stored.  Weights (one term) and activations
+// differ in nothing else.
 #include <hip/hip_fp16.h>
 
 #include <algorithm>
