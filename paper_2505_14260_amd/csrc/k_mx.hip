@@ -460,11 +460,13 @@ MSD_DEV f32x4 mfma_mx(i32x4 w, i32x4 x, f32x4 acc, int ws, int xs, int byte) {
 // eight waves the groups of K in turn, straight from memory to registers, D - 1 tiles
 // ahead, with no barrier on the way.  Their sums meet in LDS: of waves w and w + 4
 // first, then of the four.  Eight waves share K so that few columns still fill the
-// chip's memory queues, and each reads 1 KB of W in a row.  Bound by W's bytes: 10 rows by
-// 32,000 x 4,096 (71 MB) in 13 us, 5.5 TB/s; by 4,096 x 4,096 (8.9 MB) in 4.4.
+// chip's memory queues, and each reads 1 KB of W in a row.  Up to 16 rows two workgroups
+// share a CU (128 registers, so fewer tiles ahead; 10 x 152,064 x 3,584: 62 us with one).
+// Bound by W's bytes: 10 rows by 152,064 x 3,584 (290 MB) in 50 us, 5.8 TB/s; by 4,096 x
+// 4,096 (8.9 MB) in 4.4.
 constexpr int SPLIT_WAVES = 8;
 template <int MT, int CT, int TX, int TYPE>
-__global__ __launch_bounds__(64 * SPLIT_WAVES, 2) void k_mx_split(ProductArgs a, int n_ct) {
+__global__ __launch_bounds__(64 * SPLIT_WAVES, MT == 1 ? 4 : 2) void k_mx_split(ProductArgs a, int n_ct) {
   constexpr int NW = SPLIT_WAVES, U = MT * CT;
   __shared__ f32x4 sh[NW / 2][U][64];
   const int lane = threadIdx.x & 63;
@@ -487,7 +489,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES, 2) void k_mx_split(ProductArgs a,
     wc[c] = a.wc + u * tiles_pitch(nkt);
     ws[c] = a.ws + u * scales_pitch(groups);
   }
-  constexpr int D = MT * TX + CT <= 6 ? 4 : 2;  // tiles in registers
+  constexpr int D = MT * TX + CT <= 5 ? 4 : 2;  // tiles in registers
   i32x4 fx[D][MT][TX], fw[D][CT];
   int sx[MT][TX], sw[CT], sxn[MT][TX], swn[CT];
   // tile kt along K; those past the last repeat it, with scales of zero
@@ -860,14 +862,17 @@ struct ProductPlan {
 
 // Picks the kernel with the least estimated time (us), from the workgroups W on 256
 // CUs and the groups g of 512 columns of K:
-//  split  2 + l, or from W > 256 on the longer of that and 2 + W c: l, what a workgroup
-//         takes alone, goes by the rounds of g over its eight waves (less for fewer groups
-//         than waves) and the pieces n that it loads per tile along K; c is its share of
-//         the memory path;
-//  tile   f + rounds of W x 4 g steps of s + the output's writing.
-// On the 208 products that the constants were fitted to (11 weights of 512 x 8192 to
-// 32000 x 4096, 1 to 3136 rows, one and two terms) the choice costs 1.2% over the best
-// kernel on average, 35% at worst (128 x 4608 x 3584: 13.6 us for 10.1).
+//  split  1.5 + the longer of l and, for W > 256, the CU with most workgroups times its
+//         256 c: l, what a workgroup takes alone, goes by the rounds of g over its eight
+//         waves (less for fewer groups than waves) and the pieces n that it loads per tile
+//         along K; c is its share of the memory path;
+//  tile   f + rounds of W x 4 g steps of s + the output's writing, or W's bytes at the
+//         5 TB/s that these kernels read (4.6 to 4.9 measured, the split kernel 5.8).
+// On the 377 products that the constants were fitted to (15 weights of 512 x 8192 to
+// 152064 x 3584, 1 to 12288 rows, one and two terms) the choice costs 0.8% over the best
+// kernel on average, 18% at worst (1536 x 4096 x 11008, one term: 59 us for 50).  With W
+// itself in place of the fullest CU's workgroups and no limit on the tile kernels' reading
+// (on 285 of them) it was 1.9% and 36%.
 ProductPlan plan_product(int M, int N, int g, int terms) {
   ProductPlan best{};
   float best_us = 0.f;
@@ -876,24 +881,25 @@ ProductPlan plan_product(int M, int N, int g, int terms) {
   };
   const int MT = M <= 16 ? 1 : M <= 32 ? 2 : 4;
   for (int CT : {1, 2, 4}) {
-    const float W = (float)((M + 16 * MT - 1) / (16 * MT)) * ((N + 16 * CT - 1) / (16 * CT));
+    const size_t W = (size_t)((M + 16 * MT - 1) / (16 * MT)) * ((N + 16 * CT - 1) / (16 * CT));
     const int n = MT * terms + CT;
     const float rounds = g >= SPLIT_WAVES ? (g + SPLIT_WAVES - 1) / SPLIT_WAVES
                                           : 0.4f + 0.6f * g / SPLIT_WAVES;
-    const float l = rounds * (0.4f * n + 0.4f * CT - 0.3f) + 0.2f * MT * CT;
-    const float c = 1e-3f * (g * (0.22f * n + 0.5f * CT + 0.11f) + 0.8f * MT * CT);
-    take(2.f + (W <= 256.f ? l : std::max(l, W * c)), {MT, CT, 0, 0});
+    const float l = rounds * (0.24f * n + 0.76f * CT + 0.52f) + 0.13f * MT * CT;
+    const float c = 1e-3f * (g * (0.26f * n + 0.155f * CT + 0.08f) + 0.69f * MT * CT);
+    take(1.5f + (W <= 256 ? l : std::max(l, (float)((W + 255) / 256) * 256.f * c)), {MT, CT, 0, 0});
   }
   const struct {
     int BM, BN;
     float f, s[2];
-  } tiles[] = {{64, 128, 4.f, {0.198f, 0.267f}},
-               {128, 256, 6.5f, {0.55f, 0.79f}},
-               {256, 256, 9.f, {0.78f, 1.24f}}};
+  } tiles[] = {{64, 128, 4.f, {0.214f, 0.28f}},
+               {128, 256, 10.8f, {0.522f, 0.748f}},
+               {256, 256, 5.9f, {1.09f, 1.49f}}};
+  const float read = 2.f + (float)N * g * GROUP * (0.53125e-6f / 5.f);
   for (const auto& t : tiles) {
     const size_t W = (size_t)((M + t.BM - 1) / t.BM) * ((N + t.BN - 1) / t.BN);
-    take(t.f + (float)((W + 255) / 256) * 4 * g * t.s[terms - 1] + (float)M * N * 0.9e-6f,
-         {0, 0, t.BM, t.BN});
+    const float us = t.f + (float)((W + 255) / 256) * 4 * g * t.s[terms - 1] + (float)M * N * 0.35e-6f;
+    take(std::max(us, read), {0, 0, t.BM, t.BN});
   }
   return best;
 }
