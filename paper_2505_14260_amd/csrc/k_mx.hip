@@ -589,7 +589,9 @@ MSD_DEV constexpr int vmcnt_imm(int n) { return 0x0f70 | (n & 15) | ((n >> 4) <<
 // The buffers are arrays of their own and the loads into them buffer loads: the
 // compiler then knows that reads of one need not wait for loads into another.  One
 // barrier per step: before it every wave waits for its own loads into the next buffer;
-// later loads stay in flight.
+// later loads stay in flight.  With four buffers a step's loads go between its matrix
+// instructions (640 x 4,096 x 11,008: 41 us, 43 with all of them first); with two, first:
+// the step's end waits for them (3,136 x 4,096 x 11,008: 83 us, 99 in between).
 // Raw buffer loads check voffset against the record count less soffset, so soffset
 // stays inside the buffer: row and column tiles past the last and tiles past K
 // (voffset 2^31) read zeros.
@@ -707,10 +709,12 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void k_mx_tile(ProductArgs a, in
   // Step i of a group (known when compiled), tile kt along K.
   const auto step = [&](int i, int kt) {
     const i32x4 *const b = buf(i), *const bn = buf(i + 1);
+    if (!PRE) {
 #pragma unroll
-    for (int q = 0; q < XL; ++q) load1(buf(i + NB - 1), q, kt + NB - 1);
-    __builtin_amdgcn_sched_barrier(0);
-    if (!PRE) first(b, i);
+      for (int q = 0; q < XL; ++q) load1(buf(i + NB - 1), q, kt + NB - 1);
+      __builtin_amdgcn_sched_barrier(0);
+      first(b, i);
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int m = u / TX, tt = u % TX;
@@ -722,6 +726,10 @@ __global__ __launch_bounds__(64 * RW * CW, OCC) void k_mx_tile(ProductArgs a, in
       if (PRE) {
 #pragma unroll
         for (int j = u * WN / U; j < (u + 1) * WN / U; ++j) fw[(i + 1) & 1][j] = bn[wo + j * 64];
+      }
+      if (PRE) {
+#pragma unroll
+        for (int q = u * XL / U; q < (u + 1) * XL / U; ++q) load1(buf(i + NB - 1), q, kt + NB - 1);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -870,7 +878,8 @@ struct ProductPlan {
 //         5 TB/s that these kernels read (4.6 to 4.9 measured, the split kernel 5.8).
 // On the 377 products that the constants were fitted to (15 weights of 512 x 8192 to
 // 152064 x 3584, 1 to 12288 rows, one and two terms) the choice costs 0.8% over the best
-// kernel on average, 18% at worst (1536 x 4096 x 11008, one term: 59 us for 50).  With W
+// kernel on average, 18% at worst (1536 x 4096 x 11008, one term: 59 us for 50; before the
+// 64 x 128 kernel became up to 6% faster, for which its two rates are 4% lower).  With W
 // itself in place of the fullest CU's workgroups and no limit on the tile kernels' reading
 // (on 285 of them) it was 1.9% and 36%.
 ProductPlan plan_product(int M, int N, int g, int terms) {
@@ -892,7 +901,7 @@ ProductPlan plan_product(int M, int N, int g, int terms) {
   const struct {
     int BM, BN;
     float f, s[2];
-  } tiles[] = {{64, 128, 4.f, {0.214f, 0.28f}},
+  } tiles[] = {{64, 128, 4.f, {0.205f, 0.268f}},
                {128, 256, 10.8f, {0.522f, 0.748f}},
                {256, 256, 5.9f, {1.09f, 1.49f}}};
   const float read = 2.f + (float)N * g * GROUP * (0.53125e-6f / 5.f);
