@@ -382,7 +382,8 @@ class Engine:
         self.bufs_t = [torch.empty(n, dtype=torch.uint8, device=self.dev)
                        for n in (tkv, tkv, dkv, dkv, ws, pw)]
         self.bufs = Buffers(*[b.data_ptr() for b in self.bufs_t])
-        self.stream = torch.cuda.current_stream(self.dev).cuda_stream
+        self.torch_stream = torch.cuda.current_stream(self.dev)
+        self.stream = self.torch_stream.cuda_stream
         self.ctx = msd_create(self.desc, self.lim, self.tw, self.dw, self.bufs, self.stream)
         self.draft_mx = None
         self.set_draft_input(visual_input)
@@ -407,8 +408,11 @@ class Engine:
             msd_set_draft_mx(self.ctx, None)
             return
         if self.draft_mx is None:
-            self.draft_mx = self.torch.empty(msd_draft_mx_bytes(self.desc),
-                                             dtype=self.torch.uint8, device=self.dev)
+            # on the engine's stream, which fills it: a block of the current stream may
+            # still be in use there
+            with self.torch.cuda.stream(self.torch_stream):
+                self.draft_mx = self.torch.empty(msd_draft_mx_bytes(self.desc),
+                                                 dtype=self.torch.uint8, device=self.dev)
         msd_set_draft_mx(self.ctx, self.draft_mx.data_ptr())
 
     def train_accumulate(self, seq, tokens, is_visual, visual_bits):
