@@ -24,8 +24,10 @@
  *    Only msd_prefill and the two acceptance calls wait for the stream (to
  *    return host outputs).  A context serves one stream and is not thread-safe.
  *  - Return value: MSD_OK (0) or a negative MSD_ERR_*; msd_last_error()
- *    returns a message for the last failure on that context (or of
- *    msd_create when ctx is NULL).
+ *    returns a message for the last failure on that context (when ctx is NULL:
+ *    the process's last failure without a context, as of msd_create, or the
+ *    calling thread's if its own last one was of an msd_mx_* call).  The text
+ *    for NULL stays until the thread's next call of the library.
  */
 #ifndef MSD_H
 #define MSD_H
@@ -417,7 +419,7 @@ int msd_train_mix(int epoch, int n_epochs, int n_per_epoch, int* n_text_out, int
  * null stream), nothing is allocated and nothing is waited for, so a call may be
  * captured into a graph.  Calls on different streams or threads are independent.
  * Errors: MSD_ERR_INVALID_ARG (then nothing was enqueued), MSD_ERR_HIP; the message
- * is msd_last_error(NULL)'s on the calling thread.
+ * is msd_last_error(NULL)'s on the calling thread, and on no other.
  *
  * A row is cut into blocks of 32 values x that share a power of two,
  * s = 2^(floor(log2 max|x|) - 2) within [2^-127, 2^127]; each value is held as

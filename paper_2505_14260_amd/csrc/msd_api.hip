@@ -349,13 +349,30 @@ struct msd_ctx {
 
 namespace {
 
-thread_local std::string g_err;  // failures of calls without a context
+// Failures of calls without a context: the process's latest and, of the operators on
+// microscaled matrices, which several threads may call at once, the thread's own.
+std::mutex g_mu;  // of g_err
+std::string g_err;
+thread_local std::string mx_err;
+thread_local bool mx_failed = false;  // the thread's latest such failure is an operator's
+
+void note(const std::string& msg) {
+  const std::lock_guard<std::mutex> lock(g_mu);
+  g_err = msg;
+  mx_failed = false;
+}
 
 int fail(msd_ctx* c, int code, const std::string& msg) {
   if (c)
     c->err = msg;
   else
-    g_err = msg;
+    note(msg);
+  return code;
+}
+
+int mx_fail(int code, const std::string& msg) {
+  mx_err = msg;
+  mx_failed = true;
   return code;
 }
 
@@ -1745,7 +1762,7 @@ int msd_create(const msd_model_desc* m, const msd_limits* lim, const msd_target_
   };
   r = init();
   if (r != MSD_OK) {
-    g_err = c->err;
+    note(c->err);
     (void)hipHostFree(c->stage);
     delete c;
     return r;
@@ -1762,13 +1779,20 @@ int msd_destroy(msd_ctx* c) {
   const hipError_t e2 = hipHostFree(c->stage);
   delete c;
   if (e1 != hipSuccess || e2 != hipSuccess) {
-    g_err = std::string("msd_destroy: ") + hipGetErrorString(e1 != hipSuccess ? e1 : e2);
+    note(std::string("msd_destroy: ") + hipGetErrorString(e1 != hipSuccess ? e1 : e2));
     return MSD_ERR_HIP;
   }
   return MSD_OK;
 }
 
-const char* msd_last_error(const msd_ctx* c) { return c ? c->err.c_str() : g_err.c_str(); }
+const char* msd_last_error(const msd_ctx* c) {
+  if (c) return c->err.c_str();
+  if (mx_failed) return mx_err.c_str();
+  thread_local std::string copy;  // another thread may fail while this one reads
+  const std::lock_guard<std::mutex> lock(g_mu);
+  copy = g_err;
+  return copy.c_str();
+}
 
 int msd_seq_len(const msd_ctx* c, int seq) {
   if (!c || seq < 0 || seq >= c->lim.max_batch) return -1;
@@ -2293,14 +2317,14 @@ constexpr size_t MX_MAX_TILES = (size_t)1 << 22;   // 16 x 16 output tiles
 
 // The sizes of a quantised matrix.
 int mx_shape(const msd_mx* q, MxMat* out) {
-  if (!q) return fail(nullptr, MSD_ERR_INVALID_ARG, "null quantised matrix");
+  if (!q) return mx_fail(MSD_ERR_INVALID_ARG, "null quantised matrix");
   if (q->rows < 0 || q->rows > MX_MAX_ROWS || q->cols < 1 || q->cols > MX_MAX_COLS ||
       (size_t)q->rows * mx_groups(q->cols) > MX_MAX_GROUPS)
-    return fail(nullptr, MSD_ERR_INVALID_ARG, "quantised matrix: rows or cols out of range");
+    return mx_fail(MSD_ERR_INVALID_ARG, "quantised matrix: rows or cols out of range");
   if (q->layout != MSD_MX_ROWS && q->layout != MSD_MX_WEIGHT)
-    return fail(nullptr, MSD_ERR_INVALID_ARG, "quantised matrix: unknown layout");
+    return mx_fail(MSD_ERR_INVALID_ARG, "quantised matrix: unknown layout");
   if (q->terms < 1 || q->terms > (q->layout == MSD_MX_WEIGHT ? 1 : 2))
-    return fail(nullptr, MSD_ERR_INVALID_ARG, "quantised matrix: terms must be 1, or 2 in rows");
+    return mx_fail(MSD_ERR_INVALID_ARG, "quantised matrix: terms must be 1, or 2 in rows");
   *out = MxMat{q->codes_d, q->scales_d, q->rows, q->cols, q->terms, q->layout == MSD_MX_WEIGHT};
   return MSD_OK;
 }
@@ -2310,8 +2334,8 @@ int mx_mat(const msd_mx* q, MxMat* out) {
   TRY(mx_shape(q, out));
   if (q->rows && (!q->codes_d || !q->scales_d || ((uintptr_t)q->codes_d & 15) ||
                   ((uintptr_t)q->scales_d & 15)))
-    return fail(nullptr, MSD_ERR_INVALID_ARG,
-                "quantised matrix: buffers must be given and 16-byte aligned");
+    return mx_fail(MSD_ERR_INVALID_ARG,
+                   "quantised matrix: buffers must be given and 16-byte aligned");
   return MSD_OK;
 }
 
@@ -2324,12 +2348,12 @@ struct Span {
 // A float matrix of a call: its type, pointer and row distance.
 int mx_float(const void* p, int type, size_t ld, int rows, int cols, Span* out) {
   if (type != MSD_F32 && type != MSD_BF16 && type != MSD_F16)
-    return fail(nullptr, MSD_ERR_INVALID_ARG, "unknown float type");
+    return mx_fail(MSD_ERR_INVALID_ARG, "unknown float type");
   const size_t sz = type == MSD_F32 ? 4 : 2;
   if (ld < (size_t)cols || ld > ((size_t)1 << 40) / sz / std::max(rows, 1))
-    return fail(nullptr, MSD_ERR_INVALID_ARG, "row distance below the columns, or matrix too large");
+    return mx_fail(MSD_ERR_INVALID_ARG, "row distance below the columns, or matrix too large");
   if (rows && (!p || (uintptr_t)p % sz))
-    return fail(nullptr, MSD_ERR_INVALID_ARG, "null or misaligned matrix");
+    return mx_fail(MSD_ERR_INVALID_ARG, "null or misaligned matrix");
   *out = Span{p, rows ? ((size_t)(rows - 1) * ld + cols) * sz : 0};
   return MSD_OK;
 }
@@ -2341,15 +2365,21 @@ int mx_disjoint(std::initializer_list<Span> writes, std::initializer_list<Span> 
   };
   for (const Span* w = writes.begin(); w != writes.end(); ++w) {
     for (const Span* v = writes.begin(); v != w; ++v)
-      if (meet(*w, *v)) return fail(nullptr, MSD_ERR_INVALID_ARG, "outputs overlap");
+      if (meet(*w, *v)) return mx_fail(MSD_ERR_INVALID_ARG, "outputs overlap");
     for (const Span& r : reads)
-      if (meet(*w, r)) return fail(nullptr, MSD_ERR_INVALID_ARG, "an output overlaps an input");
+      if (meet(*w, r)) return mx_fail(MSD_ERR_INVALID_ARG, "an output overlaps an input");
   }
   return MSD_OK;
 }
 
 Span codes_of(const MxMat& q) { return {q.codes, mx_code_bytes(q)}; }
 Span scales_of(const MxMat& q) { return {q.scales, mx_scale_bytes(q)}; }
+
+int mx_launched() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? (int)MSD_OK
+                         : mx_fail(MSD_ERR_HIP, std::string("kernel launch: ") + hipGetErrorString(e));
+}
 
 }  // namespace
 
@@ -2370,8 +2400,7 @@ int msd_mx_quantize(const void* src_d, int type, size_t ld, const msd_mx* q, voi
   TRY(mx_float(src_d, type, ld, m.rows, m.cols, &s));
   TRY(mx_disjoint({codes_of(m), scales_of(m)}, {s}));
   launch_mx_quantise(src_d, type, ld, m, (hipStream_t)stream);
-  LAUNCHED(nullptr);
-  return MSD_OK;
+  return mx_launched();
 }
 
 int msd_mx_dequantize(const msd_mx* q, void* dst_d, int type, size_t ld, void* stream) {
@@ -2381,8 +2410,7 @@ int msd_mx_dequantize(const msd_mx* q, void* dst_d, int type, size_t ld, void* s
   TRY(mx_float(dst_d, type, ld, m.rows, m.cols, &s));
   TRY(mx_disjoint({s}, {codes_of(m), scales_of(m)}));
   launch_mx_dequantise(m, dst_d, type, ld, (hipStream_t)stream);
-  LAUNCHED(nullptr);
-  return MSD_OK;
+  return mx_launched();
 }
 
 int msd_mx_resid_norm(const void* x_d, size_t ldx, const void* y_d, size_t ldy, void* sum_d,
@@ -2392,15 +2420,15 @@ int msd_mx_resid_norm(const void* x_d, size_t ldx, const void* y_d, size_t ldy, 
   Span x, y{nullptr, 0}, s{nullptr, 0};
   TRY(mx_mat(q, &m));
   if (m.weight || m.terms != 2 || m.cols > MAX_D_MODEL)
-    return fail(nullptr, MSD_ERR_INVALID_ARG,
-                "norm: wants two terms in rows of at most 8192 columns");
+    return mx_fail(MSD_ERR_INVALID_ARG,
+                   "norm: wants two terms in rows of at most 8192 columns");
   if (!(eps >= 0.f) || !std::isfinite(eps))
-    return fail(nullptr, MSD_ERR_INVALID_ARG, "norm: eps must be finite and not negative");
+    return mx_fail(MSD_ERR_INVALID_ARG, "norm: eps must be finite and not negative");
   TRY(mx_float(x_d, type, ldx, m.rows, m.cols, &x));
   if (y_d) TRY(mx_float(y_d, type, ldy, m.rows, m.cols, &y));
   if (sum_d) TRY(mx_float(sum_d, type, lds, m.rows, m.cols, &s));
   if (!gain_d || (uintptr_t)gain_d & 1)
-    return fail(nullptr, MSD_ERR_INVALID_ARG, "norm: null or misaligned gain");
+    return mx_fail(MSD_ERR_INVALID_ARG, "norm: null or misaligned gain");
   const Span g{gain_d, 2 * (size_t)m.cols};
   const Span none{nullptr, 0};
   // the sum may take the place of an operand: each thread reads before it writes
@@ -2409,8 +2437,7 @@ int msd_mx_resid_norm(const void* x_d, size_t ldx, const void* y_d, size_t ldy, 
   TRY(mx_disjoint({s}, {on_x ? none : x, on_y ? none : y, g}));
   launch_mx_norm(x_d, ldx, y_d, ldy, sum_d, lds, type, static_cast<const uint16_t*>(gain_d), eps, m,
                  (hipStream_t)stream);
-  LAUNCHED(nullptr);
-  return MSD_OK;
+  return mx_launched();
 }
 
 int msd_mx_swiglu(const void* gate_d, size_t ldg, const void* up_d, size_t ldu, int type,
@@ -2419,13 +2446,12 @@ int msd_mx_swiglu(const void* gate_d, size_t ldg, const void* up_d, size_t ldu, 
   Span g, u;
   TRY(mx_mat(q, &m));
   if (m.weight || m.terms != 2)
-    return fail(nullptr, MSD_ERR_INVALID_ARG, "swiglu: wants two terms in rows");
+    return mx_fail(MSD_ERR_INVALID_ARG, "swiglu: wants two terms in rows");
   TRY(mx_float(gate_d, type, ldg, m.rows, m.cols, &g));
   TRY(mx_float(up_d, type, ldu, m.rows, m.cols, &u));
   TRY(mx_disjoint({codes_of(m), scales_of(m)}, {g, u}));
   launch_mx_swiglu(gate_d, ldg, up_d, ldu, type, m, (hipStream_t)stream);
-  LAUNCHED(nullptr);
-  return MSD_OK;
+  return mx_launched();
 }
 
 int msd_mx_product(const msd_mx* x, const msd_mx* w, void* out_d, int type, size_t ld,
@@ -2435,15 +2461,14 @@ int msd_mx_product(const msd_mx* x, const msd_mx* w, void* out_d, int type, size
   TRY(mx_mat(x, &a));
   TRY(mx_mat(w, &b));
   if (a.weight || !b.weight || a.cols != b.cols)
-    return fail(nullptr, MSD_ERR_INVALID_ARG,
-                "product: wants rows and a weight of the same number of columns");
+    return mx_fail(MSD_ERR_INVALID_ARG,
+                   "product: wants rows and a weight of the same number of columns");
   if ((size_t)((a.rows + 15) / 16) * ((b.rows + 15) / 16) > MX_MAX_TILES)
-    return fail(nullptr, MSD_ERR_INVALID_ARG, "product: too many output tiles");
+    return mx_fail(MSD_ERR_INVALID_ARG, "product: too many output tiles");
   TRY(mx_float(out_d, type, ld, b.rows ? a.rows : 0, std::max(b.rows, 1), &o));
   TRY(mx_disjoint({o}, {codes_of(a), scales_of(a), codes_of(b), scales_of(b)}));
   launch_mx_product(a, b, out_d, type, ld, (hipStream_t)stream);
-  LAUNCHED(nullptr);
-  return MSD_OK;
+  return mx_launched();
 }
 
 }  // extern "C"
