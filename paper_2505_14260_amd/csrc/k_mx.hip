@@ -381,20 +381,27 @@ __global__ __launch_bounds__(NT) void k_mx_norm(const void* x, size_t ldx, const
 }
 
 // -------------------------------------------------------------- swiglu ----
-// silu(g) u = g u f, f = 1 / (1 + e^-g), from t = e^-|g|: r = 1 / (1 + t) (1 ulp) for
-// g >= 0, t r below.  The larger of |g| and |u| takes f first: where that product leaves
-// float32's normal range, the whole one is below what 4 bits hold (2^-129).  Below -80
-// f is t = e^(128 - |g|) E E, which e^-|g| reaches through float32's denormals only
-// (from -87 on) though g u f may still be a normal value: 128 - |g| is exact, E = e^-64,
-// and an E goes to either factor.  (640 x 11,008 float32: 13.5 us with either form.)
-MSD_DEV float swiglu(float g, float u) {
-  const float a = fabsf(g), b = fabsf(u);
-  const bool far = g < -80.f;
-  const float t = expf(far ? 128.f - a : -a);
-  const float r = __builtin_amdgcn_rcpf(1.f + t);
-  const float E = far ? 1.6038109e-28f : 1.f;
-  const float f = far ? t : g < 0.f ? t * r : r;
-  return (a > b ? g : u) * E * f * (a > b ? u : g) * E;
+// silu(g) u = g u r for g >= 0, g u t r below, with t = e^-|g| = f 2^n and r = 1 / (1 + t)
+// (1 ulp).  f is the hardware's 2^x (1 ulp) of -|g| log2(e) - n, the product in two parts;
+// past |g| = 1000 all of it is zero.  2^n takes its place last, so that neither t nor
+// silu(g) has to be a normal float32 value for g u t r to be right: g f is exact for a
+// denormal g (f = 1), and u r rounds a denormal u by 2^-150, which g <= 17 (r < 1) cannot
+// make more than 2^-145 (the smallest 4-bit step is 2^-128).  HALVES: half of 2^n before
+// the product with u r, which overflows without it where |u| is 2^119 and more; calls
+// without come first, and again with it where the value is not finite (640 x 11,008
+// float32: 13.2 us, 12.9 with expf and silu(g) rounded first, 13.7 with HALVES at once).
+template <bool HALVES>
+MSD_DEV float silu_times(float g, float u) {
+  const float a = -__builtin_amdgcn_fmed3f(fabsf(g), 0.f, 1000.f);
+  const float L = 0x1.715476p+0f, M = 0x1.4ae0cp-26f;  // log2(e) = L + M
+  const float m = rintf(a * L);
+  const float f = __builtin_amdgcn_exp2f(fmaf(a, M, fmaf(a, L, -m)));
+  const int n = (int)m;
+  const float r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_ldexpf(f, n));
+  const int e = g < 0.f ? n : 0, h = HALVES ? e >> 1 : 0;
+  float w = g < 0.f ? g * f : g;
+  if (HALVES) w = __builtin_amdgcn_ldexpf(w, h);
+  return __builtin_amdgcn_ldexpf(w * (u * r), e - h);
 }
 
 // Activations' split (k_mx_rows).  Bound by memory: 640 x 11,008 float32, 64 MB with the
@@ -410,9 +417,19 @@ __global__ __launch_bounds__(ROW_THREADS) void k_mx_swiglu(const void* gate, con
   float g[8], u[8];
   load8<TYPE>(gate, row * ldg + k0, F - k0, g);
   load8<TYPE>(up, row * ldu + k0, F - k0, u);
+  float v[8];
+  uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) g[i] = swiglu(g[i], u[i]);
-  put_rows<2>(o, row, k0, g);
+  for (int i = 0; i < 8; ++i) {
+    v[i] = silu_times<false>(g[i], u[i]);
+    top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  }
+  if (__builtin_expect(__any(top >= 0x7F800000u), 0)) {  // out of the common path's way
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (!__builtin_isfinite(v[i])) v[i] = silu_times<true>(g[i], u[i]);
+  }
+  put_rows<2>(o, row, k0, v);
 }
 
 // ------------------------------------------------------------- product ----

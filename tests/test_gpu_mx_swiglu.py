@@ -1,11 +1,13 @@
 """silu(gate) * up where a factor of it leaves float32's normal range and the product
 does not: against the float64 oracle, as test_swiglu of test_gpu_mx.py.
 
-The error is 2^-21 for gates from -80 up, as counted there (the exponential and the
-reciprocal within 2^-23 each; 1 + e and three products rounded once each).  Below, e^-|g|
-is taken as e^(128 - |g|) E E with E = e^-64: 128 - |g| is exact (|g| >= 64), the
-exponential within 2^-23, each E rounded (2^-24), and four products rounded once each:
-2^-23 + 2 * 2^-24 + 4 * 2^-24 = 2^-21 as well.
+The error is at most 2^-21, as counted there, in units of 2^-23: e^-|g| = f 2^n has f from
+the hardware's 2^x (1) of an argument below 1/2 with two roundings of 2^-26 (0.17), and
+three products are rounded once each (1.5).  For g below zero the reciprocal of 1 + t and
+its argument add 1 + 0.5 at most; where t is near 1 (the reciprocal near 1/2, where 1 ulp
+is 1) half of f's error cancels in t / (1 + t): 0.59 + 1 + 0.25 + 1.5; where t vanishes
+the reciprocal is near 1 (1 ulp is 0.5): 1.17 + 0.5 + 0.5 + 1.5 = 3.67, below 4.  2^n is
+exact where the value is a normal number.
 """
 import numpy as np
 import pytest
@@ -86,3 +88,13 @@ def test_infinities_and_zeros():
     v = values(q).reshape(len(pairs), 32)
     # a NaN or an infinity makes its block NaN; the others are zero
     assert np.isnan(v[:6]).all() and (v[6:] == 0).all()
+
+
+def test_overflow_before_the_exponential():
+    """|g u| past float32's largest value, |silu(g) u| below it."""
+    g = gen(7)
+    gate = -40 * torch.rand(ROWS, COLS, generator=g)
+    up = 3e38 * (2 * torch.rand(ROWS, COLS, generator=g) - 1)
+    ref = check(gate, up)
+    assert np.abs(ref).max() < 3e38
+    assert ((gate.double() * up.double()).abs() > 3.5e38).double().mean() > 0.5
