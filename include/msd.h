@@ -226,9 +226,9 @@ int msd_use_caller_weights(msd_ctx* ctx, int enable);
  * msd_trace_enable records no GEMMs of a 4-bit draft.
  * mx_weights_d: device memory of msd_draft_mx_bytes bytes, 256-byte aligned, valid until
  * msd_destroy or a call with another buffer.  A draft tree of 26 nodes, 7B-shaped:
- * 0.53 ms (0.86 in bfloat16).
- * Errors: MSD_ERR_INVALID_ARG (NULL context, misaligned, or d_model, ffn_dim or n_heads *
- * head_dim too small for the workspace to hold the quantised rows: below 96), MSD_ERR_HIP.
+ * 0.54 ms (0.87 in bfloat16).
+ * Errors: MSD_ERR_INVALID_ARG (NULL context, misaligned, or d_model or ffn_dim too small for
+ * the workspace to hold the quantised rows, which may be so below 96), MSD_ERR_HIP.
  */
 int msd_draft_mx_bytes(const msd_model_desc* m, size_t* bytes);
 int msd_set_draft_mx(msd_ctx* ctx, void* mx_weights_d);

@@ -404,8 +404,8 @@ MSD_DEV float silu_times(float g, float u) {
   return __builtin_amdgcn_ldexpf(w * (u * r), e - h);
 }
 
-// Activations' split (k_mx_rows).  Bound by memory: 640 x 11,008 float32, 64 MB with the
-// codes, in 13.5 us (4.8 TB/s); 10 rows 4.2 us.
+// Activations' split (k_mx_rows).  Bound by memory, near its arithmetic's time: 640 x 11,008
+// float32, 64 MB with the codes, in 13.2 us (4.9 TB/s); 10 rows 3.7 us.
 template <int TYPE>
 __global__ __launch_bounds__(ROW_THREADS) void k_mx_swiglu(const void* gate, const void* up,
                                                            size_t ldg, size_t ldu, int rows, int F,
@@ -489,7 +489,8 @@ MSD_DEV f32x4 mfma_mx(i32x4 w, i32x4 x, f32x4 acc, int ws, int xs, int byte) {
 // chip's memory queues, and each reads 1 KB of W in a row.  Up to 16 rows two workgroups
 // share a CU (128 registers, so fewer tiles ahead; 10 x 152,064 x 3,584: 62 us with one).
 // Bound by W's bytes: 10 rows by 152,064 x 3,584 (290 MB) in 50 us, 5.8 TB/s; by 4,096 x
-// 4,096 (8.9 MB) in 4.4.
+// 4,096 (8.9 MB) in 4.4.  Over few columns and more rows by X, which every workgroup reads:
+// 64 x 4,096 x 11,008 in 16.4 us, 190 MB of X for 24 MB of W.
 template <int MT, int CT, int TX, int TYPE>
 __global__ __launch_bounds__(64 * SPLIT_WAVES, MT == 1 ? 4 : 2) void k_mx_split(ProductArgs a, int n_ct) {
   constexpr int NW = SPLIT_WAVES, U = MT * CT;
