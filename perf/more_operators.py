@@ -1,0 +1,291 @@
+"""The operators on rows of logits, as cases that can be timed and compared.
+
+A case is one pass through one operator on logits [rows, cols], cols being the
+vocabulary, as an LM head leaves them:
+
+  top      the k largest logits of a row in order, their ids, and the row's log-sum-exp
+  sample   one token a row under a temperature, top-k, top-p and min-p, from given
+           uniform numbers, and its log-probability
+  filter   the logits with what those settings remove at -inf, and how many stay
+  distill  a loss against a teacher's top logits, and its gradient: in one pass
+           ("fused", the rows' weights known before), or forward and then backward
+
+Where `own` is false `run` computes them from elementary torch operations.
+"""
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+# --- the cases ---------------------------------------------------------------------------
+
+
+def listed():
+    return [
+        # log-probabilities of one answered token
+        dict(name="top-token", op="top", rows=1, cols=32000, type="f32", pad=0, k=10),
+        # the record of a teacher over a 640-row training sequence
+        dict(name="top-teacher", op="top", rows=639, cols=32000, type="f32", pad=0, k=64),
+        # an odd vocabulary inside wider rows
+        dict(name="top-odd", op="top", rows=61, cols=50021, type="f16", pad=3, k=200),
+        # the record over a 1,152-row sequence of a wide vocabulary
+        dict(name="top-long", op="top", rows=1151, cols=152064, type="bf16", pad=0, k=128),
+        # the next token of one sequence, temperature alone
+        dict(name="sample-token", op="sample", rows=1, cols=32000, type="f32", pad=0,
+             temperature=1.0, top_k=0, top_p=1.0, min_p=0.0),
+        # a served batch with the usual settings together
+        dict(name="sample-batch", op="sample", rows=64, cols=152064, type="bf16", pad=0,
+             temperature=0.8, top_k=50, top_p=0.9, min_p=0.0),
+        # every node of the largest batch of trees, top-p alone: any number of tokens may stay
+        dict(name="sample-nucleus", op="sample", rows=512, cols=152064, type="f32", pad=0,
+             temperature=1.0, top_k=0, top_p=0.95, min_p=0.0),
+        # a verified 27-node tree before its acceptance
+        dict(name="filter-tree", op="filter", rows=27, cols=32000, type="f32", pad=0,
+             temperature=0.7, top_k=0, top_p=0.9, min_p=0.0),
+        # eight verified 61-node trees, min-p and a high temperature
+        dict(name="filter-batch", op="filter", rows=488, cols=152064, type="f32", pad=0,
+             temperature=1.5, top_k=0, top_p=0.98, min_p=0.02),
+        # a short training sequence
+        dict(name="distill-short", op="distill", rows=26, cols=32000, type="f32", pad=0, k=16,
+             temperature=1.0, fused=True),
+        # a 640-row training sequence
+        dict(name="distill-step", op="distill", rows=639, cols=32000, type="f32", pad=0, k=64,
+             temperature=1.0, fused=True),
+        # a 1,152-row sequence of a wide vocabulary, the gradient asked for later
+        dict(name="distill-long", op="distill", rows=1151, cols=152064, type="bf16", pad=0, k=100,
+             temperature=2.0, fused=False),
+    ]
+
+
+MOST = 1151 * 152064  # logits of a drawn case
+
+
+def _log(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    op = rng.choice(["top", "sample", "filter", "distill"])
+    t = rng.choice(["f32", "bf16", "f16"])
+    cols = _log(rng, 200, 152064)
+    most = MOST if t != "f32" else MOST // 2
+    if op in ("sample", "filter"):
+        most = min(most, 488 * 152064)
+    case = dict(op=op, rows=_log(rng, 1, min(3136, most // cols)), cols=cols, type=t,
+                pad=rng.choice([0, 0, 1, 8, 40]))
+    if op == "top":
+        return dict(case, k=_log(rng, 1, min(256, cols)))
+    if op == "distill":
+        return dict(case, k=_log(rng, 1, min(256, cols)), temperature=rng.choice([1.0, 1.5, 2.0]),
+                    fused=rng.random() < 0.5)
+    return dict(case, temperature=round(rng.uniform(0.3, 2.0), 2),
+                top_k=rng.choice([0, 0, _log(rng, 1, cols)]),
+                top_p=rng.choice([1.0, round(rng.uniform(0.1, 0.999), 3)]),
+                min_p=rng.choice([0.0, 0.0, round(rng.uniform(0.001, 0.5), 3)]))
+
+
+def work(case):
+    R, V, s = case["rows"], case["cols"], 4 if case["type"] == "f32" else 2
+    if case["op"] == "top":
+        return dict(bytes=R * V * s + R * (8 * case["k"] + 4), flops=4.0 * R * V)
+    if case["op"] == "sample":
+        return dict(bytes=R * V * s + 12 * R, flops=(2.0 if 0 < case["top_k"] <= 256 else 14.0) * R * V)
+    if case["op"] == "filter":
+        return dict(bytes=2 * R * V * s + 4 * R, flops=14.0 * R * V)
+    return dict(bytes=2 * R * V * s + R * (8 * case["k"] + 12), flops=8.0 * R * V)
+
+
+# --- inputs ------------------------------------------------------------------------------
+
+
+def _inputs(case, seed):
+    """Logits as a model's head leaves them: a broad bulk, and in each row a few
+    tokens far above it, more of them in some rows than in others."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    R, V, t = case["rows"], case["cols"], DTYPES[case["type"]]
+
+    def uniform(*shape):
+        return torch.rand(*shape, generator=g, device="cuda")
+
+    def rows(bulk):
+        n = min(V, 40)
+        x = torch.randn(R, V, generator=g, device="cuda") * bulk
+        # one in each of n equal stretches: no place twice
+        some = ((torch.arange(n, device="cuda") + uniform(R, n) * 0.999) * (V // n)).long()
+        x.scatter_(1, some, uniform(R, n) * uniform(R, 1) * 12 + 2)
+        return x
+
+    x = rows(2.0)
+    d = {}
+    if case["op"] == "distill":
+        # a student near its teacher; the teacher's record is in descending order
+        teacher = x + torch.randn(R, V, generator=g, device="cuda") * 0.7
+        d["values"], ids = torch.topk(teacher, case["k"], dim=1)
+        d["ids"] = ids.to(torch.int32)
+        d["grad"] = 0.5 + uniform(R)  # weights of the rows in the loss
+        del teacher
+    elif case["op"] == "sample":
+        d["uniforms"] = uniform(R)
+    wide = torch.zeros(R, V + case["pad"], dtype=t, device="cuda")
+    wide[:, :V] = x
+    return dict(d, x=wide[:, :V])
+
+
+def prepare(case, seed):
+    st = dict(_inputs(case, seed), case=case)
+    if not own:
+        return st
+    # the outputs that a program keeps
+    R, V = case["rows"], case["cols"]
+    f32 = dict(dtype=torch.float32, device="cuda")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    if case["op"] == "top":
+        st.update(top=torch.empty(R, case["k"], **f32), at=torch.empty(R, case["k"], **i32),
+                  lse=torch.empty(R, **f32))
+    elif case["op"] == "sample":
+        st.update(tokens=torch.empty(R, **i32), logprobs=torch.empty(R, **f32))
+    elif case["op"] == "filter":
+        st.update(out=torch.empty(R, V, dtype=st["x"].dtype, device="cuda"),
+                  kept=torch.empty(R, **i32))
+    else:
+        st.update(loss=torch.empty(R, **f32), lse=torch.empty(R, **f32),
+                  dx=torch.empty(R, V, dtype=st["x"].dtype, device="cuda"))
+    return st
+
+
+# --- the operators -----------------------------------------------------------------------
+
+
+def _settings(case):
+    return dict(temperature=case["temperature"], top_k=case["top_k"], top_p=case["top_p"],
+                min_p=case["min_p"])
+
+
+def _choice(case, x):
+    """Weights exp((x - max) / T) in 64 bits (a token lies next to the border of what
+    is kept or drawn), and which tokens stay."""
+    V = x.shape[1]
+    z = x.double()
+    w = torch.exp((z - z.amax(1, keepdim=True)) / case["temperature"])
+    down, order = torch.sort(w, dim=1, descending=True, stable=True)
+    n_k = case["top_k"] if 0 < case["top_k"] < V else V
+    down[:, n_k:] = 0
+    n = torch.full((x.shape[0], 1), n_k, device=x.device)
+    if case["top_p"] < 1:
+        mass = torch.cumsum(down, 1)
+        n = torch.minimum(n, (mass < case["top_p"] * mass[:, -1:]).sum(1, keepdim=True) + 1)
+    n = torch.minimum(n, (down >= case["min_p"]).sum(1, keepdim=True))
+    first = torch.arange(V, device=x.device) < n
+    return w, torch.zeros_like(first).scatter_(1, order, first), n[:, 0]
+
+
+def run(st):
+    if own:
+        return _run_own(st)
+    case, x = st["case"], st["x"]
+    if case["op"] == "top":
+        z = x.float()
+        m = z.amax(1, keepdim=True)
+        lse = m[:, 0] + torch.log(torch.exp(z - m).sum(1))
+        top, at = torch.sort(z, dim=1, descending=True, stable=True)
+        k = case["k"]
+        return dict(top=top[:, :k].contiguous(), at=at[:, :k].to(torch.int32), lse=lse)
+    if case["op"] == "filter":
+        _, keep, n = _choice(case, x)
+        return dict(out=torch.where(keep, x, float("-inf")), kept=n.to(torch.int32))
+    if case["op"] == "sample":
+        w, keep, _ = _choice(case, x)
+        mass = torch.cumsum(w * keep, 1)
+        total = mass[:, -1:]
+        token = (mass <= st["uniforms"].double()[:, None] * total).sum(1, keepdim=True)
+        logprob = torch.log(w.gather(1, token) / total)
+        return dict(tokens=token[:, 0].to(torch.int32), logprobs=logprob[:, 0].float())
+    T = case["temperature"]
+    z = x.float() / T
+    m = z.amax(1, keepdim=True)
+    e = torch.exp(z - m)
+    total = e.sum(1, keepdim=True)
+    lse = m + torch.log(total)
+    t = st["values"] / T
+    t = t - t[:, :1]
+    lq = t - torch.log(torch.exp(t).sum(1, keepdim=True))
+    q = torch.exp(lq)
+    ids = st["ids"].long()
+    loss = (q * (lq - (z.gather(1, ids) - lse))).sum(1)
+    dx = (e / total).scatter_add_(1, ids, -q) * (st["grad"][:, None] / T)
+    return dict(loss=loss, lse=lse[:, 0], dx=dx.to(x.dtype))
+
+
+def _run_own(st):
+    from paper_2505_14260_amd import logits
+    case, x = st["case"], st["x"]
+    if case["op"] == "top":
+        logits.top(x, st["top"], st["at"], st["lse"])
+        return dict(top=st["top"], at=st["at"], lse=st["lse"])
+    if case["op"] == "filter":
+        logits.filter(x, st["out"], st["kept"], **_settings(case))
+        return dict(out=st["out"], kept=st["kept"])
+    if case["op"] == "sample":
+        logits.sample(x, st["uniforms"], st["tokens"], st["logprobs"], **_settings(case))
+        return dict(tokens=st["tokens"], logprobs=st["logprobs"])
+    teacher = (st["ids"], st["values"], case["temperature"])
+    if case["fused"]:
+        logits.distill(x, *teacher, st["loss"], st["lse"], st["grad"], st["dx"])
+    else:
+        logits.distill(x, *teacher, st["loss"], st["lse"])
+        logits.distill_backward(x, *teacher, st["lse"], st["grad"], st["dx"])
+    return dict(loss=st["loss"], lse=st["lse"], dx=st["dx"])
+
+
+# --- the definition in 64 bits -----------------------------------------------------------
+
+
+def _exact_sample(case, z, u):
+    """Token by token from the ranked list of each row."""
+    p = torch.softmax(z / case["temperature"], dim=1)
+    # ranks: by probability, then by id (a stable sort of the negated logits)
+    order = torch.argsort(-z, dim=1, stable=True)
+    ranked = p.gather(1, order)
+    n = ranked.shape[1]
+    place = torch.arange(n, device=z.device)[None, :]
+    if case["top_k"]:
+        ranked = torch.where(place < case["top_k"], ranked, 0.0)
+    alive = ranked > 0
+    before = torch.cumsum(ranked, 1) - ranked
+    if case["top_p"] < 1:
+        alive &= before < case["top_p"] * ranked.sum(1, keepdim=True)
+    alive &= ranked >= case["min_p"] * ranked[:, :1]
+    if u is None:
+        return alive, order
+    q = torch.zeros_like(p).scatter_(1, order, torch.where(alive, ranked, 0.0))
+    q = q / q.sum(1, keepdim=True)
+    at = torch.searchsorted(torch.cumsum(q, 1), u[:, None], right=True).clamp(max=n - 1)
+    return at, torch.log(q.gather(1, at))
+
+
+def exact(case, seed):
+    d = _inputs(case, seed)
+    z = d["x"].double()
+    if case["op"] == "top":
+        at = torch.argsort(-z, dim=1, stable=True)[:, :case["k"]]
+        return dict(top=z.gather(1, at), at=at.to(torch.int32), lse=torch.logsumexp(z, 1))
+    if case["op"] == "filter":
+        alive, order = _exact_sample(case, z, None)
+        keep = torch.zeros_like(alive).scatter_(1, order, alive)
+        return dict(out=z.masked_fill(~keep, -math.inf), kept=alive.sum(1).to(torch.int32))
+    if case["op"] == "sample":
+        at, logprob = _exact_sample(case, z, d["uniforms"].double())
+        return dict(tokens=at[:, 0].to(torch.int32), logprobs=logprob[:, 0])
+    T = case["temperature"]
+    lp = torch.log_softmax(z / T, dim=1)
+    lq = torch.log_softmax(d["values"].double() / T, dim=1)
+    ids = d["ids"].long()
+    lse = torch.logsumexp(z / T, 1)
+    loss = (lq.exp() * (lq - lp.gather(1, ids))).sum(1)
+    dx = lp.exp_()
+    dx.scatter_add_(1, ids, -lq.exp())
+    return dict(loss=loss, lse=lse, dx=dx * (d["grad"].double() / T)[:, None])
