@@ -237,7 +237,7 @@ def _run_own(st):
         logits.distill(x, *teacher, st["loss"], st["lse"], st["grad"], st["dx"])
     else:
         logits.distill(x, *teacher, st["loss"], st["lse"])
-        logits.distill_backward(x, *teacher, st["lse"], st["grad"], st["dx"])
+        logits.distill_backward(x, *teacher, st["grad"], st["dx"])
     return dict(loss=st["loss"], lse=st["lse"], dx=st["dx"])
 
 
