@@ -26,8 +26,8 @@
  *  - Return value: MSD_OK (0) or a negative MSD_ERR_*; msd_last_error()
  *    returns a message for the last failure on that context (when ctx is NULL:
  *    the process's last failure without a context, as of msd_create, or the
- *    calling thread's if its own last one was of an msd_mx_* call).  The text
- *    for NULL stays until the thread's next call of the library.
+ *    calling thread's if its own last one was of an msd_mx_* or msd_logits_*
+ *    call).  The text for NULL stays until the thread's next call of the library.
  */
 #ifndef MSD_H
 #define MSD_H
@@ -482,6 +482,84 @@ int msd_mx_swiglu(const void* gate_d, size_t ldg, const void* up_d, size_t ldu, 
  */
 int msd_mx_product(const msd_mx* x, const msd_mx* w, void* out_d, int type, size_t ld,
                    void* stream);
+
+/*
+ * Operators on rows of logits, as msd_verify or any LM head leaves them.  They need no
+ * context and follow the msd_mx_* calls in everything said there of streams, graphs,
+ * threads, errors and float matrices: logits_d [rows][cols] of `type`, rows ld values
+ * apart.  rows 0 .. 2^21, cols (the vocabulary) 1 .. 2^18.  Every other array is
+ * contiguous, [rows] or [rows][k].  No buffer that a call writes may overlap another
+ * of its buffers, but that the logits written (filter) or their gradient (distill) may
+ * take the logits' place (same pointer and row distance).  A call's result is the same
+ * every time.
+ *
+ * Tokens of a row are ranked by logit, then by id, the lowest first.  In all of these
+ * but the distillation's student a NaN counts as -inf, and -0 equals 0.
+ */
+
+/* The k (1 .. min(256, cols)) first of every row in order, their values and ids, and
+ * lse = log sum exp(x) (NULL: not wanted): values - lse are log-probabilities.  -inf
+ * values rank last; a row of them has lse -inf. */
+int msd_logits_top(const void* logits_d, int type, size_t ld, int rows, int cols, int k,
+                   float* values_d, int32_t* ids_d, float* lse_d, void* stream);
+
+/*
+ * Which tokens of a row stay, with weights w = exp((x - max x) / temperature):
+ *   top_k   the first top_k (0: all);
+ *   top_p   of those, the fewest first ones whose weights are together at least top_p
+ *           of all of theirs (0 < top_p <= 1; 1: all);
+ *   min_p   those with w >= min_p (0 .. 1; 0: all).
+ * Those with a logit of -inf never do; any other row keeps its first token.  temperature 0
+ * keeps the first token alone; else it is positive and finite.  Weights are computed in 64 bits and summed as
+ * whole numbers of 2^-45, so that borders do not depend on an order of summation.
+ */
+typedef struct msd_sampling {
+  double temperature, top_p, min_p;
+  int32_t top_k;
+} msd_sampling;
+
+/* One token of every row, drawn from those that stay with probabilities in the ratio of
+ * their weights: the first id whose running sum of weights (in the order of ids) exceeds
+ * uniforms_d[row] (0 <= u < 1; what is not is taken as the nearest) of the whole sum.
+ * logprobs_d (or NULL): the log of its probability.  A row without tokens: -1 and -inf. */
+int msd_logits_sample(const void* logits_d, int type, size_t ld, int rows, int cols,
+                      const msd_sampling* how, const float* uniforms_d, int32_t* tokens_d,
+                      float* logprobs_d, void* stream);
+
+/* out_d = the logits that stay as they are, -inf for the others, of the same type;
+ * kept_d (or NULL): how many stayed.  msd_accept_sample on filtered logits at the same
+ * temperature emits tokens of the filtered distribution. */
+int msd_logits_filter(const void* logits_d, int type, size_t ld, int rows, int cols,
+                      const msd_sampling* how, void* out_d, size_t ldo, int32_t* kept_d,
+                      void* stream);
+
+/*
+ * Distillation from a teacher's top logits.  The teacher's record of a row is k (1 ..
+ * 256) entries, ids_d and values_d [rows][k], as msd_logits_top writes them (any order;
+ * an id outside [0, cols) is no entry, so a row may have fewer, and an id may come
+ * twice).  With q the softmax of a row's values / temperature over its entries and p
+ * the softmax of its logits / temperature over all cols (temperature positive and
+ * finite):
+ *   loss = sum of q (log q - log p);
+ *   lse  = log sum exp(x / temperature);
+ *   dlogits_d = grad / temperature (p - q), of the logits' type, q summed over the
+ *               entries of an id: the gradient of the sum of grad_d[row] loss[row].
+ * loss_d, lse_d and the pair grad_d, dlogits_d may each be NULL, not all; grad_d and
+ * dlogits_d go together.  loss and gradient come in one pass over the logits when both
+ * are asked for.  A row without entries (or with values of -inf only) has loss 0 and
+ * gradient 0.  Where the teacher has mass and the student's logit is -inf the loss is
+ * infinite (the gradient is not).  A NaN, or an infinite value other than -inf, makes
+ * its row NaN; so does a student's row of -inf.
+ */
+typedef struct msd_teacher {
+  const int32_t* ids_d;
+  const float* values_d;
+  int32_t k;
+  double temperature;
+} msd_teacher;
+int msd_logits_distill(const void* logits_d, int type, size_t ld, int rows, int cols,
+                       const msd_teacher* teacher, float* loss_d, float* lse_d,
+                       const float* grad_d, void* dlogits_d, size_t ldd, void* stream);
 
 /*
  * Diagnostic for measurement tools: one kernel that reads `bytes` of the

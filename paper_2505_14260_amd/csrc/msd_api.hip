@@ -350,7 +350,7 @@ struct msd_ctx {
 namespace {
 
 // Failures of calls without a context: the process's latest and, of the operators on
-// microscaled matrices, which several threads may call at once, the thread's own.
+// matrices and logits, which several threads may call at once, the thread's own.
 std::mutex g_mu;  // of g_err
 std::string g_err;
 thread_local std::string mx_err;
@@ -2468,6 +2468,117 @@ int msd_mx_product(const msd_mx* x, const msd_mx* w, void* out_d, int type, size
   TRY(mx_float(out_d, type, ld, b.rows ? a.rows : 0, std::max(b.rows, 1), &o));
   TRY(mx_disjoint({o}, {codes_of(a), scales_of(a), codes_of(b), scales_of(b)}));
   launch_mx_product(a, b, out_d, type, ld, (hipStream_t)stream);
+  return mx_launched();
+}
+
+}  // extern "C"
+
+namespace {
+
+constexpr int LOGITS_MAX_ROWS = 1 << 21;  // (a launch has fewer than 2^32 threads)
+
+int logits_float(const void* p, int type, size_t ld, int rows, int cols, Span* out) {
+  if (rows < 0 || rows > LOGITS_MAX_ROWS || cols < 1 || cols > LOGITS_MAX_COLS)
+    return mx_fail(MSD_ERR_INVALID_ARG, "logits: rows or cols out of range");
+  return mx_float(p, type, ld, rows, cols, out);
+}
+
+// An array of n 4-byte values (null: none).
+int logits_array(const void* p, size_t n, bool needed, Span* out) {
+  if ((needed && n && !p) || ((uintptr_t)p & 3))
+    return mx_fail(MSD_ERR_INVALID_ARG, "logits: null or misaligned array");
+  *out = Span{p, p ? 4 * n : 0};
+  return MSD_OK;
+}
+
+int logits_choice(const msd_sampling* s, LogitsChoice* out) {
+  if (!s) return mx_fail(MSD_ERR_INVALID_ARG, "logits: null settings");
+  if (!(s->temperature >= 0) || !std::isfinite(s->temperature))
+    return mx_fail(MSD_ERR_INVALID_ARG, "logits: temperature must be finite and not negative");
+  if (s->top_k < 0 || !(s->top_p > 0 && s->top_p <= 1) || !(s->min_p >= 0 && s->min_p <= 1))
+    return mx_fail(MSD_ERR_INVALID_ARG,
+                   "logits: wants top_k >= 0, 0 < top_p <= 1 and 0 <= min_p <= 1");
+  const bool greedy = s->temperature == 0;
+  const double T = greedy ? 1 : s->temperature;
+  *out = LogitsChoice{M_LOG2E / T, s->top_p, s->min_p > 0 ? T * std::log(s->min_p) : -INFINITY,
+                      greedy ? 1 : s->top_k};
+  return MSD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int msd_logits_top(const void* logits_d, int type, size_t ld, int rows, int cols, int k,
+                   float* values_d, int32_t* ids_d, float* lse_d, void* stream) {
+  Span x, v, i, l;
+  TRY(logits_float(logits_d, type, ld, rows, cols, &x));
+  if (k < 1 || k > std::min(LOGITS_TOP_MAX, cols))
+    return mx_fail(MSD_ERR_INVALID_ARG, "logits: k must be 1 .. min(256, cols)");
+  TRY(logits_array(values_d, (size_t)rows * k, true, &v));
+  TRY(logits_array(ids_d, (size_t)rows * k, true, &i));
+  TRY(logits_array(lse_d, rows, false, &l));
+  TRY(mx_disjoint({v, i, l}, {x}));
+  launch_logits_top(logits_d, type, ld, rows, cols, k, values_d, ids_d, lse_d, (hipStream_t)stream);
+  return mx_launched();
+}
+
+int msd_logits_sample(const void* logits_d, int type, size_t ld, int rows, int cols,
+                      const msd_sampling* how, const float* uniforms_d, int32_t* tokens_d,
+                      float* logprobs_d, void* stream) {
+  Span x, u, t, l;
+  LogitsChoice c;
+  TRY(logits_float(logits_d, type, ld, rows, cols, &x));
+  TRY(logits_choice(how, &c));
+  TRY(logits_array(uniforms_d, rows, true, &u));
+  TRY(logits_array(tokens_d, rows, true, &t));
+  TRY(logits_array(logprobs_d, rows, false, &l));
+  TRY(mx_disjoint({t, l}, {x, u}));
+  launch_logits_sample(logits_d, type, ld, rows, cols, c, uniforms_d, tokens_d, logprobs_d,
+                       (hipStream_t)stream);
+  return mx_launched();
+}
+
+int msd_logits_filter(const void* logits_d, int type, size_t ld, int rows, int cols,
+                      const msd_sampling* how, void* out_d, size_t ldo, int32_t* kept_d,
+                      void* stream) {
+  Span x, o, n;
+  LogitsChoice c;
+  TRY(logits_float(logits_d, type, ld, rows, cols, &x));
+  TRY(logits_choice(how, &c));
+  TRY(logits_float(out_d, type, ldo, rows, cols, &o));
+  TRY(logits_array(kept_d, rows, false, &n));
+  TRY(mx_disjoint({n}, {x}));
+  const bool in_place = out_d == logits_d && ldo == ld;
+  TRY(mx_disjoint({o, n}, {in_place ? Span{nullptr, 0} : x}));
+  launch_logits_filter(logits_d, type, ld, rows, cols, c, out_d, ldo, kept_d, (hipStream_t)stream);
+  return mx_launched();
+}
+
+int msd_logits_distill(const void* logits_d, int type, size_t ld, int rows, int cols,
+                       const msd_teacher* teacher, float* loss_d, float* lse_d,
+                       const float* grad_d, void* dlogits_d, size_t ldd, void* stream) {
+  Span x, ids, vals, l, e, g, dx{nullptr, 0};
+  TRY(logits_float(logits_d, type, ld, rows, cols, &x));
+  if (!teacher || teacher->k < 1 || teacher->k > LOGITS_TOP_MAX)
+    return mx_fail(MSD_ERR_INVALID_ARG, "distill: wants a teacher of 1 .. 256 entries a row");
+  if (!(teacher->temperature > 0) || !std::isfinite(teacher->temperature))
+    return mx_fail(MSD_ERR_INVALID_ARG, "distill: temperature must be positive and finite");
+  if (rows && ((!grad_d != !dlogits_d) || (!loss_d && !lse_d && !dlogits_d)))
+    return mx_fail(MSD_ERR_INVALID_ARG,
+                   "distill: wants an output, and the rows' weights with the gradient");
+  TRY(logits_array(teacher->ids_d, (size_t)rows * teacher->k, true, &ids));
+  TRY(logits_array(teacher->values_d, (size_t)rows * teacher->k, true, &vals));
+  TRY(logits_array(loss_d, rows, false, &l));
+  TRY(logits_array(lse_d, rows, false, &e));
+  TRY(logits_array(grad_d, rows, false, &g));
+  if (dlogits_d) TRY(logits_float(dlogits_d, type, ldd, rows, cols, &dx));
+  TRY(mx_disjoint({l, e}, {x, ids, vals, g}));
+  const bool in_place = dlogits_d == logits_d && ldd == ld;
+  TRY(mx_disjoint({dx, l, e}, {in_place ? Span{nullptr, 0} : x, ids, vals, g}));
+  const LogitsTeacher t{teacher->ids_d, teacher->values_d, teacher->k, 1 / teacher->temperature};
+  launch_logits_distill(logits_d, type, ld, rows, cols, t, loss_d, lse_d, grad_d, dlogits_d, ldd,
+                        (hipStream_t)stream);
   return mx_launched();
 }
 

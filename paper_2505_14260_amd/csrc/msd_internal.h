@@ -434,4 +434,34 @@ void launch_mx_swiglu(const void* gate, size_t ldg, const void* up, size_t ldu, 
 void launch_mx_product(const MxMat& x, const MxMat& w, void* out, int type, size_t ldo,
                        hipStream_t st);
 
+// ------------------------------------------------------ rows of logits ----
+// Operators on logits [rows][cols] of a float type (MX_F32, MX_BF16, MX_F16), rows ld
+// values apart (k_logits.hip).
+constexpr int LOGITS_TOP_MAX = 256;      // entries of a row's top logits
+constexpr int LOGITS_MAX_COLS = 1 << 18;
+struct LogitsChoice {
+  double c;      // log2(e) / temperature
+  double top_p;  // 1: all
+  double min_d;  // temperature * log(min_p); -inf: all
+  int top_k;     // 0: all
+};
+struct LogitsTeacher {
+  const int* ids;       // [rows][k]; outside [0, cols): no entry
+  const float* values;  // [rows][k]
+  int k;
+  double inv_t;
+};
+void launch_logits_top(const void* x, int type, size_t ld, int rows, int cols, int k, float* values,
+                       int* ids, float* lse, hipStream_t st);
+void launch_logits_sample(const void* x, int type, size_t ld, int rows, int cols,
+                          const LogitsChoice& how, const float* uniforms, int* tokens,
+                          float* logprobs, hipStream_t st);
+void launch_logits_filter(const void* x, int type, size_t ld, int rows, int cols,
+                          const LogitsChoice& how, void* out, size_t ldo, int* kept,
+                          hipStream_t st);
+// any of loss, lse and dx may be null
+void launch_logits_distill(const void* x, int type, size_t ld, int rows, int cols,
+                           const LogitsTeacher& t, float* loss, float* lse, const float* grad,
+                           void* dx, size_t ldd, hipStream_t st);
+
 }  // namespace msd

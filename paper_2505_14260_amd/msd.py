@@ -72,6 +72,18 @@ class Mx(ctypes.Structure):
                 ("layout", c_i32), ("terms", c_i32)]
 
 
+class Sampling(ctypes.Structure):
+    """Which tokens of a row of logits stay (msd_sampling)."""
+    _fields_ = [("temperature", ctypes.c_double), ("top_p", ctypes.c_double),
+                ("min_p", ctypes.c_double), ("top_k", c_i32)]
+
+
+class Teacher(ctypes.Structure):
+    """A teacher's top logits (msd_teacher)."""
+    _fields_ = [("ids_d", c_vp), ("values_d", c_vp), ("k", c_i32),
+                ("temperature", ctypes.c_double)]
+
+
 _lib = None
 
 
@@ -120,6 +132,11 @@ def lib():
                                         c_f32, P(Mx), c_vp]
         L.msd_mx_swiglu.argtypes = [c_vp, c_sz, c_vp, c_sz, ctypes.c_int, P(Mx), c_vp]
         L.msd_mx_product.argtypes = [P(Mx), P(Mx), c_vp, ctypes.c_int, c_sz, c_vp]
+        rows = [c_vp, ctypes.c_int, c_sz, ctypes.c_int, ctypes.c_int]
+        L.msd_logits_top.argtypes = rows + [ctypes.c_int, c_vp, c_vp, c_vp, c_vp]
+        L.msd_logits_sample.argtypes = rows + [P(Sampling), c_vp, c_vp, c_vp, c_vp]
+        L.msd_logits_filter.argtypes = rows + [P(Sampling), c_vp, c_sz, c_vp, c_vp]
+        L.msd_logits_distill.argtypes = rows + [P(Teacher), c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]
         L.msd_trace_enable.argtypes = [c_vp, ctypes.c_int, ctypes.c_int]
         L.msd_trace_read.argtypes = [c_vp, ctypes.c_int, P(TraceRec)]
         _lib = L
@@ -324,6 +341,29 @@ def msd_mx_swiglu(gate_ptr, ldg, up_ptr, ldu, type_, q: Mx, stream):
 
 def msd_mx_product(x: Mx, w: Mx, out_ptr, type_, ld, stream):
     _check(None, lib().msd_mx_product(x, w, out_ptr, type_, ld, stream))
+
+
+def msd_logits_top(logits_ptr, type_, ld, rows, cols, k, values_ptr, ids_ptr, lse_ptr, stream):
+    _check(None, lib().msd_logits_top(logits_ptr, type_, ld, rows, cols, k, values_ptr, ids_ptr,
+                                      lse_ptr, stream))
+
+
+def msd_logits_sample(logits_ptr, type_, ld, rows, cols, how: Sampling, uniforms_ptr, tokens_ptr,
+                      logprobs_ptr, stream):
+    _check(None, lib().msd_logits_sample(logits_ptr, type_, ld, rows, cols, how, uniforms_ptr,
+                                         tokens_ptr, logprobs_ptr, stream))
+
+
+def msd_logits_filter(logits_ptr, type_, ld, rows, cols, how: Sampling, out_ptr, ldo, kept_ptr,
+                      stream):
+    _check(None, lib().msd_logits_filter(logits_ptr, type_, ld, rows, cols, how, out_ptr, ldo,
+                                         kept_ptr, stream))
+
+
+def msd_logits_distill(logits_ptr, type_, ld, rows, cols, teacher: Teacher, loss_ptr, lse_ptr,
+                       grad_ptr, dlogits_ptr, ldd, stream):
+    _check(None, lib().msd_logits_distill(logits_ptr, type_, ld, rows, cols, teacher, loss_ptr,
+                                          lse_ptr, grad_ptr, dlogits_ptr, ldd, stream))
 
 
 def msd_trace_enable(ctx, capacity, kinds=0xF):
