@@ -2500,7 +2500,7 @@ int logits_choice(const msd_sampling* s, LogitsChoice* out) {
                    "logits: wants top_k >= 0, 0 < top_p <= 1 and 0 <= min_p <= 1");
   const bool greedy = s->temperature == 0;
   const double T = greedy ? 1 : s->temperature;
-  *out = LogitsChoice{M_LOG2E / T, s->top_p, s->min_p > 0 ? T * std::log(s->min_p) : -INFINITY,
+  *out = LogitsChoice{std::min(M_LOG2E / T, 1e300), s->top_p, s->min_p > 0 ? T * std::log(s->min_p) : -INFINITY,
                       greedy ? 1 : s->top_k};
   return MSD_OK;
 }
@@ -2562,8 +2562,8 @@ int msd_logits_distill(const void* logits_d, int type, size_t ld, int rows, int 
   TRY(logits_float(logits_d, type, ld, rows, cols, &x));
   if (!teacher || teacher->k < 1 || teacher->k > LOGITS_TOP_MAX)
     return mx_fail(MSD_ERR_INVALID_ARG, "distill: wants a teacher of 1 .. 256 entries a row");
-  if (!(teacher->temperature > 0) || !std::isfinite(teacher->temperature))
-    return mx_fail(MSD_ERR_INVALID_ARG, "distill: temperature must be positive and finite");
+  if (!(teacher->temperature >= 1e-6) || !std::isfinite(teacher->temperature))
+    return mx_fail(MSD_ERR_INVALID_ARG, "distill: temperature must be finite and 1e-6 at least");
   if (rows && ((!grad_d != !dlogits_d) || (!loss_d && !lse_d && !dlogits_d)))
     return mx_fail(MSD_ERR_INVALID_ARG,
                    "distill: wants an output, and the rows' weights with the gradient");
