@@ -538,8 +538,7 @@ int msd_logits_filter(const void* logits_d, int type, size_t ld, int rows, int c
  * 256) entries, ids_d and values_d [rows][k], as msd_logits_top writes them (any order;
  * an id outside [0, cols) is no entry, so a row may have fewer, and an id may come
  * twice).  With q the softmax of a row's values / temperature over its entries and p
- * the softmax of its logits / temperature over all cols (temperature finite, 1e-6 at
- * least):
+ * the softmax of its logits / temperature over all cols (temperature 1e-6 .. 1e6):
  *   loss = sum of q (log q - log p);
  *   lse  = log sum exp(x / temperature);
  *   dlogits_d = grad / temperature (p - q), of the logits' type, q summed over the

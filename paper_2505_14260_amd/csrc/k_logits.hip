@@ -77,11 +77,33 @@ MSD_DEV void lower(u32x4& u, int e, uint32_t h) {
     u[e / 2] = e & 1 ? (u[e / 2] & 0xFFFFu) | h << 16 : (u[e / 2] & 0xFFFF0000u) | h;
 }
 
+// A unit of E values, rounded by the hardware's conversions.
+template <int TYPE>
+MSD_DEV u32x4 pack(const float (&v)[Type<TYPE>::E]) {
+  u32x4 u;
+  if constexpr (TYPE == MX_F32) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = __float_as_uint(v[e]);
+  } else {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (TYPE == MX_BF16)
+        u[e] = __builtin_bit_cast(uint32_t, b2{(__bf16)v[2 * e], (__bf16)v[2 * e + 1]});
+      else
+        u[e] = __builtin_bit_cast(uint32_t, h2{(_Float16)v[2 * e], (_Float16)v[2 * e + 1]});
+    }
+  }
+  return u;
+}
+
 // A row of V logits over LB threads, in tiles of a unit of 16 bytes each: unit j of a
 // thread begins at element (j LB + thread) E; places past V hold -inf.
 template <int TYPE, int LB_>
 struct Row {
   static constexpr int T = TYPE, LB = LB_, E = Type<TYPE>::E, TILE = LB * E, W = LB / 64;
+  static constexpr bool HELD = false;
   typedef typename Type<TYPE>::unit unit;
   const char* p;
   int V;
@@ -102,25 +124,27 @@ struct Row {
       if (i + e < V) lower<TYPE>(u, e, bits_at<TYPE>(p, i + e));
     return u;
   }
-  // f(j, id, unit) for every tile in order, read from memory, AHEAD tiles at a time.
+  // f(j, id, unit) for every tile in order, read from memory, the next AHEAD tiles
+  // under way while f works on these.
   template <int AHEAD, class F>
   MSD_DEV void each(F f) const {
-    const int full = V / TILE, n = (V + TILE - 1) / TILE;
-    for (int j = 0; j < n; j += AHEAD) {
+    const int full = V / TILE;
+    u32x4 next[AHEAD], last = Type<TYPE>::NINF;
+#pragma unroll
+    for (int b = 0; b < AHEAD; ++b) next[b] = b < full ? load(b) : last;
+    if (V % TILE) last = load_tail(full);
+    for (int j = 0; j < full; j += AHEAD) {
       u32x4 t[AHEAD];
 #pragma unroll
-      for (int b = 0; b < AHEAD; ++b)
-        if (j + b < full) t[b] = load(j + b);
-      if (full < n && full < j + AHEAD) {
-        const u32x4 last = load_tail(full);
-#pragma unroll
-        for (int b = 0; b < AHEAD; ++b)
-          if (j + b == full) t[b] = last;
+      for (int b = 0; b < AHEAD; ++b) {
+        t[b] = next[b];
+        if (j + AHEAD + b < full) next[b] = load(j + AHEAD + b);
       }
 #pragma unroll
       for (int b = 0; b < AHEAD; ++b)
-        if (j + b < n) f(j + b, id(j + b), t[b]);
+        if (j + b < full) f(j + b, id(j + b), t[b]);
     }
+    if (V % TILE) f(full, id(full), last);
   }
   MSD_DEV void store(char* o, int i, const u32x4& u) const {
     if (i + E <= V) {
@@ -137,7 +161,9 @@ struct Row {
 template <int TYPE, int LB, int U>
 struct HeldRow : Row<TYPE, LB> {
   typedef Row<TYPE, LB> Base;
-  u32x4 r[U], last;
+  static constexpr bool HELD = true;
+  static constexpr int UNITS = U;
+  mutable u32x4 r[U], last;
   MSD_DEV HeldRow(const void* base, size_t ld, int V) : Base(base, ld, V) {
     const int full = V / Base::TILE;
 #pragma unroll
@@ -149,8 +175,12 @@ struct HeldRow : Row<TYPE, LB> {
   MSD_DEV void each(F f) const {
     const int full = this->V / Base::TILE;
 #pragma unroll
-    for (int j = 0; j < U; ++j)
+    for (int j = 0; j < U; ++j) {
+      // so that no pass keeps its converted values for the next one
+      asm("" : "+v"(r[j]));
       if (j < full) f(j, this->id(j), r[j]);
+    }
+    asm("" : "+v"(last));
     if (this->V % Base::TILE) f(full, this->id(full), last);
   }
 };
@@ -179,12 +209,17 @@ MSD_DEV uint64_t place_of(uint32_t key, int id) { return ((uint64_t)key << 32) |
 // Chebyshev interpolation of (2^r - 1) / r of degree 8 (3.7e-14 off at most).
 constexpr double ONE = 0x1p45;
 struct Scale {
-  double m, c;
-  bool finite;  // an infinite maximum leaves itself alone
+  float m;
+  double c, m64;
+  bool finite;  // an infinite maximum weighs 1 and leaves nothing to the others
+  MSD_DEV Scale(float m_, double c_)
+      : m(m_), c(c_), m64(m_ < INFINITY ? m_ : 0.0), finite(m_ < INFINITY) {}
+  MSD_DEV float operator()(float x) const {  // what weighs
+    return finite ? x : x == INFINITY ? 0.f : -INFINITY;
+  }
 };
-MSD_DEV uint64_t weight(float x, const Scale& s) {
-  if (!s.finite) return x == (float)s.m ? (uint64_t)ONE : 0;
-  const double t = fmax(((double)x - s.m) * s.c, -64.0);  // (a NaN too)
+MSD_DEV uint64_t weight_of(float x, const Scale& s) {
+  const double t = fmax(((double)x - s.m64) * s.c, -64.0);  // (a NaN too)
   const double k = t + 0x1.8p52;                          // rounded in its last bits
   const double r = t - (k - 0x1.8p52);
   double q = 0x1.b63880a30e9ffp-24;
@@ -201,6 +236,7 @@ MSD_DEV uint64_t weight(float x, const Scale& s) {
   // the last bit of a double in [128, 256) is 2^-45
   return (uint64_t)(__double_as_longlong(w + 128.0) - 0x4060000000000000ll);
 }
+MSD_DEV uint64_t weight(float x, const Scale& s) { return weight_of(s(x), s); }
 
 // ------------------------------------------------------- waves and workgroups ----
 
@@ -240,14 +276,9 @@ struct Max {
   MSD_DEV uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; }
 };
 
-constexpr int LISTED = 1024;  // tokens that are ranked among each other
 constexpr int BINS = 2048;
 constexpr int SLOTS = 4;
-struct Lds {
-  uint64_t hist[BINS];    // also the weights of a list, and sums of a row's stretches
-  uint64_t list[LISTED];
-  uint64_t sorted[LOGITS_TOP_MAX];
-  int rank[LISTED];
+struct Lds {  // of every kernel
   uint64_t part[SLOTS][16];
   uint64_t found[2];
   int bin, count;
@@ -301,6 +332,29 @@ struct Group {
   }
 };
 
+// The key of a row's largest, and one that the r largest of the threads' largest reach
+// in every wave: so W r tokens at least reach it, and few more of most rows.
+struct Tops {
+  uint32_t max, floor;
+};
+template <int W>
+MSD_DEV Tops tops(uint32_t mine, int r, Group<W>& g) {
+  uint32_t least = 0;  // the first 20 bits of the r-th largest: at most that
+#pragma unroll
+  for (int b = 31; b >= 12; --b) {
+    const uint32_t up = least | 1u << b;
+    if (__popcll(__ballot(mine >= up)) >= r) least = up;
+  }
+  const uint64_t* p = g.swap((uint64_t)wave_scan(mine, 0u, Max()) << 32 | least);
+  Tops t{0, 0xFFFFFFFFu};
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    t.max = Max()(t.max, (uint32_t)(p[i] >> 32));
+    t.floor = min(t.floor, (uint32_t)p[i]);
+  }
+  return t;
+}
+
 // The last token that is kept of a row.
 struct Kept {
   uint32_t key;
@@ -315,65 +369,73 @@ struct Keeps {  // the same as values
 
 // ------------------------------------------------------------------ thresholds ----
 
-// The bin of s.hist in which the running sum reaches `want`, with the sum before it and
-// its own in s.found.  Bins ascend from bin 0 on, or descend from the last.
+// The bin of hist in which the running sum reaches `want` (of *all, for the whole, when
+// `share` of it is wanted), with the sum before it and its own in s.found.  Bins ascend
+// from bin 0 on, or descend from the last.
 template <int W, bool DOWN>
-MSD_DEV void find_bin(uint64_t want, Group<W>& g) {
-  Lds& s = g.s;
+MSD_DEV uint64_t find_bin(const uint64_t* hist, uint64_t want, double share, uint64_t* all,
+                          Group<W>& g) {
   constexpr int PER = BINS / (W * 64);
-  uint64_t h[PER], sum = 0, all;
+  uint64_t h[PER], sum = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int b = threadIdx.x * PER + i;
-    sum += h[i] = s.hist[DOWN ? BINS - 1 - b : b];
+    sum += h[i] = hist[DOWN ? BINS - 1 - b : b];
   }
-  uint64_t run = g.before(sum, &all);
+  uint64_t run = g.before(sum, all);
+  if (share > 0) {
+    want = (uint64_t)ceil((double)*all * share);
+    want = want < 1 ? 1 : want > *all ? *all : want;
+  }
   if (run < want && want <= run + sum) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       if (run < want && want <= run + h[i]) {
         const int b = threadIdx.x * PER + i;
-        s.bin = DOWN ? BINS - 1 - b : b;
-        s.found[0] = run;
-        s.found[1] = h[i];
+        g.s.bin = DOWN ? BINS - 1 - b : b;
+        g.s.found[0] = run;
+        g.s.found[1] = h[i];
       }
       run += h[i];
     }
   }
   lds_barrier();
+  return want;
 }
 
 template <int W>
-MSD_DEV void clear_bins(Lds& s) {
+MSD_DEV void clear_bins(uint64_t* hist) {
   lds_barrier();
-  for (int i = threadIdx.x; i < BINS; i += W * 64) s.hist[i] = 0;
+  for (int i = threadIdx.x; i < BINS; i += W * 64) hist[i] = 0;
   lds_barrier();
 }
 
 // The shortest prefix of the ranked row whose counts (null) or weights sum to at least
-// `want` (1 <= want <= their sum), digit by digit of the keys: for any row.
+// `want` (1 <= want <= their sum), digit by digit of the keys: for any row, in up to
+// four passes over it.
 template <class R>
-MSD_DEV Kept shortest(const R& row, const Scale* sc, uint64_t want, Group<R::W>& g) {
+MSD_DEV Kept shortest(const R& row, const Scale* sc, uint64_t want, uint64_t* hist,
+                      Group<R::W>& g) {
   Lds& s = g.s;
   uint32_t prefix = 0;  // the digits found so far
   int left = 32;        // bits below them
-  uint64_t ties = 0, each = 1;
+  uint64_t ties = 0, each = 1, all;
   while (left > 0) {
     const int bits = left > 11 ? 11 : left;
     const int low = left - bits;
-    clear_bins<R::W>(s);
-    row.template each<4>([&](int, int i, const u32x4& u) {
+    clear_bins<R::W>(hist);
+    row.template each<2>([&](int, int i, const u32x4& u) {
 #pragma unroll
       for (int e = 0; e < R::E; ++e) {
         const float x = from_bits<R::T>(lift<R::T>(u, e));
         const uint32_t k = key_of(x);
         if (i + e >= row.V || (left < 32 && (k ^ prefix) >> left)) continue;
         const uint64_t w = sc ? weight(x, *sc) : 1;
-        if (w) atomicAdd((unsigned long long*)&s.hist[(k >> low) & ((1u << bits) - 1)], w);
+        if (w) atomicAdd((unsigned long long*)&hist[(k >> low) & ((1u << bits) - 1)], w);
       }
     });
     lds_barrier();
-    find_bin<R::W, true>(want, g);
+    find_bin<R::W, true>(hist, want, 0, &all, g);
     prefix |= (uint32_t)s.bin << low;
     want -= s.found[0];
     ties = s.found[1];
@@ -384,13 +446,12 @@ MSD_DEV Kept shortest(const R& row, const Scale* sc, uint64_t want, Group<R::W>&
   if (n * each >= ties) return {prefix, row.V};
   // the n-th of them in the order of their ids
   uint64_t seen = 0;
-  row.template each<4>([&](int, int i, const u32x4& u) {
+  row.template each<1>([&](int, int i, const u32x4& u) {
     if (seen >= n) return;
     int hits = 0;
 #pragma unroll
     for (int e = 0; e < R::E; ++e)
       hits += i + e < row.V && key_of(from_bits<R::T>(lift<R::T>(u, e))) == prefix;
-    uint64_t all;
     uint64_t before = seen + g.before(hits, &all);
     seen += all;
     if (before >= n || before + hits < n) return;
@@ -403,143 +464,28 @@ MSD_DEV Kept shortest(const R& row, const Scale* sc, uint64_t want, Group<R::W>&
   return {prefix, s.bin};
 }
 
-// Tokens of the row that `takes` into s.list, in any order; their number, which may be
-// more than fit.
+// Places of the unit's tokens that `takes` at the end of a list of `room`; s.count counts
+// those that found none too.
 template <class R, class F>
-MSD_DEV int make_list(const R& row, Lds& s, F takes) {
+MSD_DEV void append(const R& row, int i, const u32x4& u, uint64_t* list, int room, Lds& s, F takes) {
+  int c = 0;
+#pragma unroll
+  for (int e = 0; e < R::E; ++e)
+    c += i + e < row.V && takes(from_bits<R::T>(lift<R::T>(u, e)), i + e);
+  if (!c) return;
+  int at = atomicAdd(&s.count, c);
+#pragma unroll
+  for (int e = 0; e < R::E; ++e) {
+    const float x = from_bits<R::T>(lift<R::T>(u, e));
+    if (i + e >= row.V || !takes(x, i + e)) continue;
+    if (at < room) list[at] = place_of(key_of(x), i + e);
+    ++at;
+  }
+}
+MSD_DEV void clear_count(Lds& s) {
   lds_barrier();
   if (threadIdx.x == 0) s.count = 0;
   lds_barrier();
-  row.template each<4>([&](int, int i, const u32x4& u) {
-#pragma unroll
-    for (int e = 0; e < R::E; ++e) {
-      const float x = from_bits<R::T>(lift<R::T>(u, e));
-      if (!takes(x, i + e) || i + e >= row.V) continue;
-      const int at = atomicAdd(&s.count, 1);
-      if (at < LISTED) s.list[at] = place_of(key_of(x), i + e);
-    }
-  });
-  lds_barrier();
-  return s.count;
-}
-
-// The first n (at most LOGITS_TOP_MAX and V) tokens of the row in order, in s.sorted.
-// A wave's r-th largest of its threads' largest, r = n / W rounded up, is reached by r
-// tokens of that wave; the least of these over the waves, so by n tokens of the row,
-// and by few more of most rows.  Those are ranked by counting.
-template <class R>
-MSD_DEV void first_tokens(const R& row, uint32_t mine, int n, Group<R::W>& g) {
-  Lds& s = g.s;
-  const int r = (n + R::W - 1) / R::W;
-  uint32_t least = 0;  // its first 20 bits: at most the r-th largest
-#pragma unroll
-  for (int b = 31; b >= 12; --b) {
-    const uint32_t up = least | 1u << b;
-    if (__popcll(__ballot(mine >= up)) >= r) least = up;
-  }
-  const uint32_t floor_key = ~g.max(~least);
-  const float at_least = of_key(floor_key);
-  int C = floor_key > KEY_NINF ? make_list(row, s, [&](float x, int) { return x >= at_least; })
-                               : make_list(row, s, [&](float, int) { return true; });
-  if (C > LISTED) {  // very many equal ones, or the largest in few threads
-    const Kept k = shortest(row, nullptr, n, g);
-    C = make_list(row, s, [&](float x, int i) {
-      const uint32_t key = key_of(x);
-      return key > k.key || (key == k.key && i <= k.id);
-    });
-  }
-  for (int i = threadIdx.x; i < C; i += R::LB) s.rank[i] = 0;
-  lds_barrier();
-  // the list in parts, so that every wave counts
-  const int pad = (C + 63) & ~63;
-  const int parts = pad < R::LB ? R::LB / pad : 1;
-  const int per = (C + parts - 1) / parts;
-  for (int i0 = threadIdx.x; i0 < pad * parts; i0 += R::LB) {
-    const int q = i0 / pad, i = i0 - q * pad;
-    if (i >= C) continue;
-    const uint64_t me = s.list[i];
-    int above = 0;
-    const int end = min(C, (q + 1) * per);
-    for (int k = q * per; k < end; ++k) above += s.list[k] > me;
-    if (above) atomicAdd(&s.rank[i], above);
-  }
-  lds_barrier();
-  for (int i = threadIdx.x; i < C; i += R::LB)
-    if (s.rank[i] < n) s.sorted[s.rank[i]] = s.list[i];
-  lds_barrier();
-}
-
-// Bins of a row's weights, 44 to a factor of two, that ascend as they fall: weights of
-// the last are below 2^-46.
-constexpr float BINS_PER_2 = 44.f;
-MSD_DEV float bin_of(float x, float m, float c) {
-  return x == m ? 0.f : fminf((m - x) * c, (float)BINS);
-}
-
-// The shortest prefix of the ranked row within `limit` whose weights sum to at least
-// top_p of that of `limit`.
-template <class R>
-MSD_DEV Kept by_weight(const R& row, const Scale& sc, double top_p, Kept limit, Group<R::W>& g) {
-  Lds& s = g.s;
-  const float m = (float)sc.m;
-  const float c = (float)(sc.c * (double)BINS_PER_2);
-  const Keeps in(limit);
-  clear_bins<R::W>(s);
-  row.template each<4>([&](int, int i, const u32x4& u) {
-#pragma unroll
-    for (int e = 0; e < R::E; ++e) {
-      const float x = from_bits<R::T>(lift<R::T>(u, e));
-      const float b = bin_of(x, m, c);
-      if (b < (float)BINS && in(x, i + e))
-        atomicAdd((unsigned long long*)&s.hist[(int)b], weight(x, sc));
-    }
-  });
-  lds_barrier();
-  uint64_t sum = 0, all;
-  for (int i = threadIdx.x; i < BINS; i += R::LB) sum += s.hist[i];
-  all = g.sum(sum);
-  uint64_t want = (uint64_t)ceil((double)all * top_p);
-  want = want < 1 ? 1 : want > all ? all : want;
-  const uint64_t whole = want;
-  find_bin<R::W, false>(want, g);
-  const float bin = (float)s.bin;
-  want -= s.found[0];
-  // the tokens of a bin are nearly alike, which tells their number
-  const bool many =
-      (double)s.found[1] > 0.9 * LISTED * ONE * (double)__builtin_amdgcn_exp2f(-bin / BINS_PER_2);
-  float sub = -1.f;
-  if (many) {  // bins of that bin
-    clear_bins<R::W>(s);
-    row.template each<4>([&](int, int i, const u32x4& u) {
-#pragma unroll
-      for (int e = 0; e < R::E; ++e) {
-        const float x = from_bits<R::T>(lift<R::T>(u, e));
-        const float b = bin_of(x, m, c);
-        if (floorf(b) == bin && in(x, i + e))
-          atomicAdd((unsigned long long*)&s.hist[(int)((b - bin) * BINS)], weight(x, sc));
-      }
-    });
-    lds_barrier();
-    find_bin<R::W, false>(want, g);
-    sub = (float)s.bin;
-    want -= s.found[0];
-  }
-  const int C = make_list(row, s, [&](float x, int i) {
-    const float b = bin_of(x, m, c);
-    return floorf(b) == bin && (sub < 0 || floorf((b - bin) * BINS) == sub) && in(x, i);
-  });
-  if (C > LISTED) return shortest(row, &sc, whole, g);
-  for (int i = threadIdx.x; i < C; i += R::LB)
-    s.hist[i] = weight(of_key((uint32_t)(s.list[i] >> 32)), sc);
-  lds_barrier();
-  for (int i = threadIdx.x; i < C; i += R::LB) {
-    const uint64_t me = s.list[i];
-    uint64_t before = 0;
-    for (int k = 0; k < C; ++k) before += s.list[k] > me ? s.hist[k] : 0;
-    if (before < want && want <= before + s.hist[i]) s.found[0] = me;
-  }
-  lds_barrier();
-  return {(uint32_t)(s.found[0] >> 32), (int)~(uint32_t)s.found[0]};
 }
 
 // The first of the values that min_p keeps: x - m >= min_d.
@@ -548,52 +494,6 @@ MSD_DEV uint32_t min_key(float m, double min_d) {
   const uint32_t k = key_of((float)least);
   return k + ((double)of_key(k) < least);  // the next one up
 }
-
-// A few tokens at most stay (0 < top_k <= LOGITS_TOP_MAX): their number, in order in
-// s.sorted, with their weights in s.hist and *all their sum.
-template <class R>
-MSD_DEV int choose_few(const R& row, uint32_t mine, const Scale& sc, const LogitsChoice& how,
-                       uint64_t* all, Group<R::W>& g) {
-  Lds& s = g.s;
-  const int n = min(how.top_k, row.V);
-  first_tokens(row, mine, n, g);
-  uint32_t key = 0;
-  uint64_t w = 0;
-  if ((int)threadIdx.x < n) {
-    key = (uint32_t)(s.sorted[threadIdx.x] >> 32);
-    w = weight(of_key(key), sc);
-    s.hist[threadIdx.x] = w;
-  }
-  uint64_t sum;
-  const uint64_t before = g.before(w, &sum);
-  bool stays = key > KEY_NINF;
-  if (how.top_p < 1) {
-    const uint64_t want = (uint64_t)ceil((double)sum * how.top_p);
-    stays = stays && (before < want || threadIdx.x == 0);
-  }
-  if (how.min_d > -INFINITY) stays = stays && key >= min_key((float)sc.m, how.min_d);
-  const int left = (int)g.sum((uint64_t)stays);
-  *all = g.sum(stays ? w : 0);
-  return left;
-}
-
-// The last token that stays.
-template <class R>
-MSD_DEV Kept choose_many(const R& row, const Scale& sc, const LogitsChoice& how, Group<R::W>& g) {
-  Kept k{KEY_NINF + 1, row.V};
-  if (how.top_k > 0 && how.top_k < row.V) {
-    const Kept t = shortest(row, nullptr, how.top_k, g);
-    if (t.key > KEY_NINF) k = t;
-  }
-  if (how.top_p < 1) k = by_weight(row, sc, how.top_p, k, g);
-  if (how.min_d > -INFINITY) {
-    const uint32_t least = min_key((float)sc.m, how.min_d);
-    if (least > k.key) k = {least, row.V};
-  }
-  return k;
-}
-
-// ------------------------------------------------------------------- operators ----
 
 // The key of the thread's largest.
 template <class R>
@@ -606,32 +506,469 @@ MSD_DEV uint32_t thread_max(const R& row) {
   return key_of(m);
 }
 
-template <class R>
-MSD_DEV Scale scale_of(float m, double c) {
-  return {(double)m, c, m < INFINITY};
+// ----------------------------------------------------------- a few first tokens ----
+
+constexpr int FEW = 1024;      // tokens that are ranked among each other,
+constexpr int FEW_PAIRS = 128; // up to so many by comparing all
+struct FewLds : Lds {
+  union {
+    uint64_t hist[BINS];
+    uint32_t base[FEW + 1];
+    uint64_t weights[LOGITS_TOP_MAX];
+  };
+  uint64_t list[FEW], other[FEW];
+  uint64_t sorted[LOGITS_TOP_MAX];
+};
+
+// s.list[0 .. C) ranked: its first n in s.sorted.  m: the row's largest, floor at most the
+// smallest value of the list.  More than a few are first brought into buckets of
+// their value, then compared within those.
+template <int LB>
+MSD_DEV void rank(FewLds& s, int C, int n, float m, float floor, Group<LB / 64>& g) {
+  if (C <= FEW_PAIRS) {
+    if ((int)threadIdx.x < C) {
+      const uint64_t me = s.list[threadIdx.x];
+      int above = 0;
+      for (int k = 0; k < C; ++k) above += s.list[k] > me;
+      if (above < n) s.sorted[above] = me;
+    }
+    lds_barrier();
+    return;
+  }
+  constexpr int PER = FEW / LB;
+  const float width = (m - floor) * (1.f / (FEW - 1));
+  const float c = width > 0 && width < INFINITY ? 1.f / width : 0.f;  // (c = inf: as good as 0)
+  const auto bucket = [&](uint64_t place) {
+    const float d = (m - of_key((uint32_t)(place >> 32))) * c;
+    return d > 0 ? (int)fminf(d, (float)(FEW - 1)) : 0;
+  };
+  for (int i = threadIdx.x; i <= FEW; i += LB) s.base[i] = 0;
+  lds_barrier();
+  uint64_t mine[PER];
+  int at[PER];
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    const int i = threadIdx.x + q * LB;
+    if (i >= C) continue;
+    mine[q] = s.list[i];
+    at[q] = (int)atomicAdd(&s.base[bucket(mine[q])], 1u);
+  }
+  lds_barrier();
+  uint32_t size[PER], sum = 0;
+#pragma unroll
+  for (int q = 0; q < PER; ++q) sum += size[q] = s.base[threadIdx.x * PER + q];
+  uint64_t all;
+  uint32_t run = (uint32_t)g.before(sum, &all);
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    s.base[threadIdx.x * PER + q] = run;
+    run += size[q];
+  }
+  if (threadIdx.x == LB - 1) s.base[FEW] = run;
+  lds_barrier();
+#pragma unroll
+  for (int q = 0; q < PER; ++q)
+    if ((int)threadIdx.x + q * LB < C) s.other[s.base[bucket(mine[q])] + at[q]] = mine[q];
+  lds_barrier();
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    if ((int)threadIdx.x + q * LB >= C) continue;
+    const int b = bucket(mine[q]);
+    const int from = s.base[b], to = s.base[b + 1];
+    int above = from;
+    if (above >= n) continue;
+    for (int k = from; k < to; ++k) above += s.other[k] > mine[q];
+    if (above < n) s.sorted[above] = mine[q];
+  }
+  lds_barrier();
 }
 
+// The first n (at most LOGITS_TOP_MAX and V) tokens of the row in order, in s.sorted:
+// those that reach a bound that n at least do, ranked.
 template <class R>
-__global__ __launch_bounds__(R::LB) void k_filter(const void* logits, size_t ld, int V,
-                                                  LogitsChoice how, void* out, size_t ldo,
-                                                  int* kept) {
-  __shared__ Lds s;
-  Group<R::W> g{s};
-  const R row(logits, ld, V);
-  char* const o = static_cast<char*>(out) + (size_t)blockIdx.x * ldo * Type<R::T>::SIZE;
-  const uint32_t mine = thread_max(row);
-  const float m = of_key(g.max(mine));
-  const Scale sc = scale_of<R>(m, how.c);
-  Kept k{0xFF800000u, -1};  // nothing: +inf of no id
-  if (m > -INFINITY) {
-    if (how.top_k > 0 && how.top_k <= LOGITS_TOP_MAX) {
-      uint64_t all;
-      const uint64_t last = s.sorted[choose_few(row, mine, sc, how, &all, g) - 1];
-      k = {(uint32_t)(last >> 32), (int)~(uint32_t)last};
-    } else {
-      k = choose_many(row, sc, how, g);
+MSD_DEV void first_tokens(const R& row, const Tops& t, int n, FewLds& s, Group<R::W>& g) {
+  const bool all = t.floor <= KEY_NINF;
+  const float at_least = all ? -INFINITY : of_key(t.floor);
+  const Row<R::T, R::LB>& mem = row;
+  uint64_t units = 0;  // of the thread's, those with one: few, and read again
+  row.template each<4>([&](int j, int, const u32x4& u) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < R::E; ++e) m = fmaxf(m, from_bits<R::T>(lift<R::T>(u, e)));
+    units |= (uint64_t)(m >= at_least) << j;
+  });
+  for (; units; units &= units - 1) {
+    const int j = __ffsll((unsigned long long)units) - 1;
+    append(mem, mem.id(j), mem.load_tail(j), s.list, FEW, s,
+           [&](float x, int) { return x >= at_least || all; });
+  }
+  lds_barrier();
+  int C = s.count;
+  if (C > FEW) {  // very many equal ones, or the largest in few threads
+    const Kept k = shortest(mem, nullptr, n, s.hist, g);
+    clear_count(s);
+    mem.template each<2>([&](int, int i, const u32x4& u) {
+      append(mem, i, u, s.list, FEW, s, [&](float x, int id) {
+        const uint32_t key = key_of(x);
+        return key > k.key || (key == k.key && id <= k.id);
+      });
+    });
+    lds_barrier();
+    C = s.count;
+  }
+  rank<R::LB>(s, C, n, of_key(t.max), at_least, g);
+}
+
+// The tokens that stay of a few at most (0 < top_k <= LOGITS_TOP_MAX): their number, in
+// order in s.sorted, with their weights in s.weights and *all their sum.
+template <class R>
+MSD_DEV int choose_few(const R& row, const Tops& t, const Scale& sc, const LogitsChoice& how,
+                       uint64_t* all, FewLds& s, Group<R::W>& g) {
+  const int n = min(how.top_k, row.V);
+  first_tokens(row, t, n, s, g);
+  uint32_t key = 0;
+  uint64_t w = 0;
+  if ((int)threadIdx.x < n) {
+    key = (uint32_t)(s.sorted[threadIdx.x] >> 32);
+    w = weight(of_key(key), sc);
+    s.weights[threadIdx.x] = w;
+  }
+  uint64_t sum;
+  const uint64_t before = g.before(w, &sum);
+  bool stays = key > KEY_NINF;
+  if (how.top_p < 1) {
+    const uint64_t want = (uint64_t)ceil((double)sum * how.top_p);
+    stays = stays && (before < want || threadIdx.x == 0);
+  }
+  if (how.min_d > -INFINITY) stays = stays && key >= min_key(sc.m, how.min_d);
+  const int left = (int)g.sum((uint64_t)stays);
+  *all = g.sum(stays ? w : 0);
+  return left;
+}
+
+// ------------------------------------------------- any number of tokens that stay ----
+
+// The pass that finds a row's largest counts its logits too, in COUNTS bins of T / 64
+// around one of them (`ref`, the largest of its first tile or of all), HEAD bins above
+// it.  With the counts and the weights of the bins' middles the border of top-p is known
+// to a bin or two.  The next pass computes the weights: those of all for their sum, those
+// that surely stay, and it lists a few thousand tokens around the estimate, among which
+// the border then has to lie.  Where it does not (rows of very many equal logits), the
+// border is found digit by digit.
+constexpr int COUNTS = 4096, HEAD = 1024;
+constexpr double COUNTS_PER_T = 64;
+constexpr int MANY = 4096;                  // the list, of up to
+constexpr int ABOVE = 1024, BELOW = 1536;   // so many before and after the border's bin
+constexpr int BORDER = 512;                 // of those that share the border's bin of the list
+constexpr int CELLS = LOGITS_MAX_COLS / 256;  // stretches of 64 units: tiles times waves
+struct ManyLds : Lds {
+  union {
+    uint64_t hist[BINS];
+    uint32_t counts[COUNTS];
+  };
+  uint64_t list[MANY];
+  uint64_t few[BORDER], few_w[BORDER];
+  uint64_t cells[CELLS];
+  int low, high;
+};
+
+struct Bins {
+  float ref, scale;
+  MSD_DEV Bins(float r, double c)
+      : ref(r), scale((float)fmin(c * (COUNTS_PER_T / M_LOG2E), 1e30)) {}
+  MSD_DEV float at(float x) const { return fmaf(x - ref, scale, (float)(COUNTS - HEAD)); }
+  MSD_DEV float edge(float b) const { return ref + (b - (float)(COUNTS - HEAD)) / scale; }
+};
+
+// The row's largest, and with `count` its counts.
+template <class R>
+MSD_DEV float largest(const R& row, double c, bool count, float* ref, ManyLds& s, Group<R::W>& g) {
+  const auto counted = [&](float x, const Bins& bins) {
+    const float b = bins.at(x);
+    if (b >= 0.f) atomicAdd(&s.counts[(int)fminf(b, (float)(COUNTS - 1))], 1u);
+  };
+  float m = -INFINITY;
+  if (count)
+    for (int i = threadIdx.x; i < COUNTS; i += R::LB) s.counts[i] = 0;
+  if constexpr (R::HELD) {
+    m = of_key(g.max(thread_max(row)));  // (its barrier: the counts are clear)
+    if (!count) return m;
+    const Bins bins(m, c);
+    row.template each<2>([&](int, int, const u32x4& u) {
+#pragma unroll
+      for (int e = 0; e < R::E; ++e) counted(from_bits<R::T>(lift<R::T>(u, e)), bins);
+    });
+    lds_barrier();
+    *ref = m;
+  } else {
+    if (!count) return of_key(g.max(thread_max(row)));
+    const u32x4 first = row.load_tail(0);
+#pragma unroll
+    for (int e = 0; e < R::E; ++e) m = fmaxf(m, from_bits<R::T>(lift<R::T>(first, e)));
+    *ref = of_key(g.max(key_of(m)));
+    const Bins bins(*ref, c);
+    row.template each<4>([&](int, int, const u32x4& u) {
+#pragma unroll
+      for (int e = 0; e < R::E; ++e) {
+        const float x = from_bits<R::T>(lift<R::T>(u, e));
+        m = fmaxf(m, x);
+        counted(x, bins);
+      }
+    });
+    m = of_key(g.max(key_of(m)));
+  }
+  return m;
+}
+
+// What is known before the weights: tokens that surely stay, and the least of the others
+// that may (+inf: none, the choice is exact).
+struct Plan {
+  Kept above;
+  float low;
+};
+
+// The estimate from the counts, bins from the last down.  least: the key that min_p asks for.
+template <class R>
+MSD_DEV Plan estimate(float ref, const Scale& sc, const LogitsChoice& how, uint32_t least,
+                      ManyLds& s, Group<R::W>& g) {
+  constexpr int PER = COUNTS / R::LB;
+  const Bins bins(ref, sc.c);
+  uint32_t n[PER], count = 0;
+  uint64_t w[PER], sum = 0, all, tokens;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int b = COUNTS - 1 - (threadIdx.x * PER + i);
+    n[i] = s.counts[b];
+    sum += w[i] = n[i] * weight(fminf(bins.edge((float)b + 0.5f), sc.m), sc);
+    count += n[i];
+  }
+  if (least > KEY_NINF + 1) {
+    // Does min_p end before top_p for certain?  Weights at the bins' edges, a hundredth
+    // of a bin wider for the rounding of a place, bound those in them.
+    const float cut = fminf(bins.at(of_key(least)) - 1.f, (float)(COUNTS - 1));
+    uint64_t most = 0, whole = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const float b = (float)(COUNTS - 1 - (threadIdx.x * PER + i));
+      whole += n[i] * weight(fminf(bins.edge(b - 0.01f), sc.m), sc);
+      if (b >= cut) most += n[i] * weight(b < COUNTS - 1 ? fminf(bins.edge(b + 1.01f), sc.m) : sc.m, sc);
+    }
+    most = g.sum(most);
+    whole = g.sum(whole);
+    if (cut >= 0.f && (double)most < (double)whole * how.top_p * (1 - 0x1p-20))
+      return {{least, 0x7FFFFFFF}, INFINITY};
+  }
+  uint64_t run = g.before(sum, &all);
+  uint32_t seen = (uint32_t)g.before(count, &tokens);
+  const uint64_t want = (uint64_t)((double)all * how.top_p);
+  if (threadIdx.x == 0) {
+    s.bin = COUNTS - 1;
+    s.count = 0;
+  }
+  lds_barrier();
+  if (run <= want && want < run + sum) {
+    uint32_t c = seen;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (run <= want && want < run + w[i]) {
+        s.bin = COUNTS - 1 - (threadIdx.x * PER + i);
+        s.count = (int)c;
+      }
+      run += w[i];
+      c += n[i];
     }
   }
+  lds_barrier();
+  const int bin = s.bin, before = s.count;
+  if (threadIdx.x == 0) s.low = s.high = bin;
+  lds_barrier();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int b = COUNTS - 1 - (threadIdx.x * PER + i);
+    if (b >= bin && (int)seen >= before - ABOVE) atomicMax(&s.high, b);
+    if (b <= bin && (int)(seen + n[i]) <= before + BELOW) atomicMin(&s.low, b);
+    seen += n[i];
+  }
+  if (threadIdx.x == 0) s.count = 0;
+  lds_barrier();
+  const float high = bins.edge((float)(s.high + 1));
+  Plan p{{0xFF800000u, -1}, bins.edge((float)s.low)};
+  if (s.high < COUNTS - 1 && high < sc.m) p.above = {key_of(high), 0x7FFFFFFF};
+  return p;
+}
+
+// The last token that stays by top-p, of which `want` of the weight is among the C listed;
+// false where it is not, or where too many are alike.
+template <int LB>
+MSD_DEV bool border(ManyLds& s, int C, const Plan& p, uint64_t want, const Scale& sc, Kept* k,
+                    Group<LB / 64>& g) {
+  const float high = fminf(of_key(p.above.key), sc.m);
+  const float width = high - p.low;
+  const float c = width > 0 ? (float)BINS / width : 0.f;
+  const auto bin_of = [&](float x) {
+    return (int)fminf(fmaxf((high - x) * c, 0.f), (float)(BINS - 1));
+  };
+  clear_bins<LB / 64>(s.hist);
+  if (threadIdx.x == 0) s.count = 0;
+  for (int i = threadIdx.x; i < C; i += LB) {
+    const float x = of_key((uint32_t)(s.list[i] >> 32));
+    atomicAdd((unsigned long long*)&s.hist[bin_of(x)], weight(x, sc));
+  }
+  lds_barrier();
+  uint64_t all;
+  find_bin<LB / 64, false>(s.hist, want, 0, &all, g);
+  if (want < 1 || want > all) return false;
+  const int bin = s.bin;
+  want -= s.found[0];
+  for (int i = threadIdx.x; i < C; i += LB) {
+    const float x = of_key((uint32_t)(s.list[i] >> 32));
+    if (bin_of(x) != bin) continue;
+    const int at = atomicAdd(&s.count, 1);
+    if (at < BORDER) {
+      s.few[at] = s.list[i];
+      s.few_w[at] = weight(x, sc);
+    }
+  }
+  lds_barrier();
+  const int n = s.count;
+  if (n > BORDER) return false;
+  for (int i = threadIdx.x; i < n; i += LB) {
+    const uint64_t me = s.few[i];
+    uint64_t before = 0;
+    for (int j = 0; j < n; ++j) before += s.few[j] > me ? s.few_w[j] : 0;
+    if (before < want && want <= before + s.few_w[i]) s.found[0] = me;
+  }
+  lds_barrier();
+  *k = {(uint32_t)(s.found[0] >> 32), (int)~(uint32_t)s.found[0]};
+  return true;
+}
+
+// What of a row's choice does not need its weights.
+struct Start {
+  Kept limit;      // of top_k
+  uint32_t least;  // of min_p
+  Plan plan;
+};
+template <class R>
+MSD_DEV Start start_many(const R& row, float ref, const Scale& sc, const LogitsChoice& how,
+                         ManyLds& s, Group<R::W>& g) {
+  const Row<R::T, R::LB>& mem = row;
+  constexpr int LAST = 0x7FFFFFFF;
+  Start st{{KEY_NINF + 1, LAST}, KEY_NINF + 1, {{0xFF800000u, -1}, 3.402823466e38f}};
+  if (how.min_d > -INFINITY) st.least = min_key(sc.m, how.min_d);
+  bool limited = false;
+  if (how.top_k > 0 && how.top_k < row.V) {
+    const Kept f = shortest(mem, nullptr, how.top_k, s.hist, g);
+    limited = f.key > KEY_NINF;
+    if (limited) st.limit = f;
+  }
+  if (how.top_p == 1) {
+    st.plan = {st.limit, INFINITY};
+    if (st.least > st.limit.key) st.plan.above = {st.least, LAST};
+  } else if (!sc.finite) {  // the infinite ones weigh alike
+    const Keeps within(st.limit);
+    uint64_t n = 0;
+    mem.template each<2>([&](int, int i, const u32x4& u) {
+#pragma unroll
+      for (int e = 0; e < R::E; ++e) {
+        const float x = from_bits<R::T>(lift<R::T>(u, e));
+        n += x == INFINITY && within(x, i + e);
+      }
+    });
+    n = g.sum(n);
+    uint64_t want = (uint64_t)ceil((double)n * how.top_p);
+    want = want < 1 ? 1 : want > n ? n : want;
+    st.plan = {shortest(mem, nullptr, want, s.hist, g), INFINITY};
+  } else if (!limited && fabsf(ref) < INFINITY) {
+    st.plan = estimate<R>(ref, sc, how, st.least, s, g);
+  }  // else nothing surely stays, and nothing is listed
+  clear_count(s);
+  return st;
+}
+
+// The pass that computes the weights of a row: their sum, where the plan is not exact, and
+// that of the tokens that surely stay, also by stretches; the tokens that may stay are
+// listed.  f is called for each unit with its values and those that surely stay.
+template <class R, class F>
+MSD_DEV void weigh(const R& row, const Scale& sc, const Start& st, bool by_cell, uint64_t* all,
+                   uint64_t* above, ManyLds& s, Group<R::W>& g, F f) {
+  const Keeps stays(st.plan.above), within(st.limit);
+  const float low = st.plan.low;
+  const bool exact = low == INFINITY, limited = st.limit.key > KEY_NINF + 1;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  uint64_t sum_all = 0, sum_above = 0;
+  row.template each<2>([&](int j, int i, const u32x4& u) {
+    float x[R::E];
+    bool in[R::E], any = false;
+    int listed = 0;
+#pragma unroll
+    for (int e = 0; e < R::E; ++e) {
+      x[e] = from_bits<R::T>(lift<R::T>(u, e));
+      if (limited && !within(x[e], i + e)) x[e] = -INFINITY;
+      any |= in[e] = stays(x[e], i + e);
+      listed += x[e] >= low && !in[e];
+    }
+    if (listed) {
+      int at = atomicAdd(&s.count, listed);
+#pragma unroll
+      for (int e = 0; e < R::E; ++e)
+        if (x[e] >= low && !in[e]) {
+          if (at < MANY) s.list[at] = place_of(key_of(x[e]), i + e);
+          ++at;
+        }
+    }
+    const bool some = __any(any);
+    if (!exact || some) {
+      float z[R::E];
+#pragma unroll
+      for (int e = 0; e < R::E; ++e) z[e] = x[e];
+      if (!sc.finite) {
+#pragma unroll
+        for (int e = 0; e < R::E; ++e) z[e] = sc(x[e]);
+      }
+      uint64_t a = 0;
+#pragma unroll
+      for (int h = 0; h < R::E; h += 4) {  // in fours: registers for their arithmetic
+        if (h) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int e = h; e < h + 4; ++e) {
+          const uint64_t w = weight_of(z[e], sc);
+          sum_all += w;
+          a += in[e] ? w : 0;
+        }
+      }
+      sum_above += a;
+      if (by_cell && some) {
+        a = wave_scan(a, (uint64_t)0, Sum());
+        if (lane == 63) s.cells[j * R::W + wave] = a;
+      }
+    }
+    f(i, u, x, in);
+  });
+  *all = exact ? 0 : g.sum(sum_all);
+  *above = g.sum(sum_above);  // (its barrier: the list is whole)
+}
+
+// The last token that stays, after a plan's weights; false where it had to be looked for
+// in passes of their own.
+template <class R>
+MSD_DEV bool decide(const R& row, const Scale& sc, const LogitsChoice& how, const Start& st,
+                    uint64_t all, uint64_t above, int C, Kept* k, ManyLds& s, Group<R::W>& g) {
+  const Row<R::T, R::LB>& mem = row;
+  uint64_t want = (uint64_t)ceil((double)all * how.top_p);
+  want = want < 1 ? 1 : want > all ? all : want;
+  const bool found = C <= MANY && want > above &&
+                     border<R::LB>(s, C, st.plan, want - above, sc, k, g);
+  if (!found) *k = shortest(mem, &sc, want, s.hist, g);
+  if (st.least > k->key) *k = {st.least, 0x7FFFFFFF};
+  return found;
+}
+
+// ------------------------------------------------------------------- operators ----
+
+// The row's logits that stay, -inf for the others; their number over the threads.
+template <class R>
+MSD_DEV uint32_t put_filtered(const R& row, char* o, Kept k) {
   const Keeps stays(k);
   uint32_t n = 0;
   row.template each<4>([&](int, int i, const u32x4& u) {
@@ -644,8 +981,84 @@ __global__ __launch_bounds__(R::LB) void k_filter(const void* logits, size_t ld,
     }
     row.store(o, i, y);
   });
-  const uint64_t all = g.sum((uint64_t)n);
-  if (kept && threadIdx.x == 0) kept[blockIdx.x] = (int)all;
+  return n;
+}
+
+template <class R>
+__global__ __launch_bounds__(R::LB) void k_filter_few(const void* logits, size_t ld, int V,
+                                                      LogitsChoice how, void* out, size_t ldo,
+                                                      int* kept) {
+  __shared__ FewLds s;
+  Group<R::W> g{s};
+  const R row(logits, ld, V);
+  char* const o = static_cast<char*>(out) + (size_t)blockIdx.x * ldo * Type<R::T>::SIZE;
+  if (threadIdx.x == 0) s.count = 0;
+  const Tops t = tops(thread_max(row), (min(how.top_k, V) + R::W - 1) / R::W, g);
+  Kept k{0xFF800000u, -1};  // nothing: +inf of no id
+  int n = 0;
+  if (t.max > KEY_NINF) {
+    uint64_t all;
+    n = choose_few(row, t, Scale(of_key(t.max), how.c), how, &all, s, g);
+    const uint64_t last = s.sorted[n - 1];
+    k = {(uint32_t)(last >> 32), (int)~(uint32_t)last};
+  }
+  put_filtered(row, o, k);
+  if (kept && threadIdx.x == 0) kept[blockIdx.x] = n;
+}
+
+template <class R>
+__global__ __launch_bounds__(R::LB) void k_filter_many(const void* logits, size_t ld, int V,
+                                                       LogitsChoice how, void* out, size_t ldo,
+                                                       int* kept) {
+  __shared__ ManyLds s;
+  Group<R::W> g{s};
+  const R row(logits, ld, V);
+  char* const o = static_cast<char*>(out) + (size_t)blockIdx.x * ldo * Type<R::T>::SIZE;
+  float ref = 0.f;
+  const float m = largest(row, how.c, how.top_p < 1, &ref, s, g);
+  Kept k{0xFF800000u, -1};  // nothing: +inf of no id
+  if (m > -INFINITY) {
+    const Scale sc(m, how.c);
+    const Start st = start_many(row, ref, sc, how, s, g);
+    k = st.plan.above;
+    if (st.plan.low < INFINITY) {
+      // the pass over a row in memory writes as well, but for one that may have to be
+      // read again
+      const bool write = !R::HELD && out != logits;
+      uint64_t all, above;
+      uint32_t n = 0;
+      weigh(row, sc, st, false, &all, &above, s, g,
+            [&](int i, const u32x4& u, const float(&x)[R::E], const bool(&in)[R::E]) {
+              if (!write) return;
+              u32x4 y = u;
+#pragma unroll
+              for (int e = 0; e < R::E; ++e) {
+                if (!(in[e] || x[e] >= st.plan.low))
+                  lower<R::T>(y, e, Type<R::T>::NINF & (R::T == MX_F32 ? ~0u : 0xFFFFu));
+                n += in[e];
+              }
+              row.store(o, i, y);
+            });
+      const int C = s.count;
+      if (decide(row, sc, how, st, all, above, C, &k, s, g) && write &&
+          (k.key < st.plan.above.key || (k.key == st.plan.above.key && k.id >= st.plan.above.id))) {
+        // of those that may stay, the ones that do not
+        const Keeps stays(k);
+        __syncthreads();
+        for (int i = threadIdx.x; i < C; i += R::LB) {
+          const int id = (int)~(uint32_t)s.list[i];
+          const bool in = stays(of_key((uint32_t)(s.list[i] >> 32)), id);
+          if (!in) put_bits<R::T>(o, id, Type<R::T>::NINF);
+          n += in;
+        }
+        const uint64_t total = g.sum((uint64_t)n);
+        if (kept && threadIdx.x == 0) kept[blockIdx.x] = (int)total;
+        return;
+      }
+    }
+  }
+  const uint64_t n = g.sum((uint64_t)put_filtered(row, o, k));
+  if (kept && threadIdx.x == 0) kept[blockIdx.x] = (int)n;
 }
 
 // The place of u in a whole of `all`.
@@ -656,74 +1069,97 @@ MSD_DEV void put_token(int id, float x, uint64_t all, const Scale& sc, int* toke
                        float* logprobs) {
   tokens[blockIdx.x] = id;
   if (logprobs)
-    logprobs[blockIdx.x] = (float)((x == (float)sc.m ? 0.0 : ((double)x - sc.m) * sc.c * M_LN2) -
+    logprobs[blockIdx.x] = (float)((x == sc.m ? 0.0 : ((double)x - sc.m64) * sc.c * M_LN2) -
                                    log((double)all * (1 / ONE)));
+}
+MSD_DEV void put_no_token(int* tokens, float* logprobs) {
+  if (threadIdx.x) return;
+  tokens[blockIdx.x] = -1;
+  if (logprobs) logprobs[blockIdx.x] = -INFINITY;
 }
 
 template <class R>
-__global__ __launch_bounds__(R::LB) void k_sample(const void* logits, size_t ld, int V,
-                                                  LogitsChoice how, const float* uniforms,
-                                                  int* tokens, float* logprobs) {
-  __shared__ Lds s;
+__global__ __launch_bounds__(R::LB) void k_sample_few(const void* logits, size_t ld, int V,
+                                                      LogitsChoice how, const float* uniforms,
+                                                      int* tokens, float* logprobs) {
+  __shared__ FewLds s;
   Group<R::W> g{s};
   const float u = uniforms[blockIdx.x];
   const R row(logits, ld, V);
-  const uint32_t mine = thread_max(row);
-  const float m = of_key(g.max(mine));
-  const Scale sc = scale_of<R>(m, how.c);
-  if (!(m > -INFINITY)) {
-    if (threadIdx.x == 0) {
-      tokens[blockIdx.x] = -1;
-      if (logprobs) logprobs[blockIdx.x] = -INFINITY;
-    }
-    return;
-  }
+  if (threadIdx.x == 0) s.count = 0;
+  const Tops t = tops(thread_max(row), (min(how.top_k, V) + R::W - 1) / R::W, g);
+  if (t.max <= KEY_NINF) return put_no_token(tokens, logprobs);
+  const Scale sc(of_key(t.max), how.c);
   uint64_t all;
-  if (how.top_k > 0 && how.top_k <= LOGITS_TOP_MAX) {
-    const int n = choose_few(row, mine, sc, how, &all, g);
-    if ((int)threadIdx.x >= n) return;
-    // the running sum in the order of the ids, of which ~ makes the lower the greater
-    const uint32_t me = (uint32_t)s.sorted[threadIdx.x];
-    uint64_t before = 0;
-    for (int i = 0; i < n; ++i) before += (uint32_t)s.sorted[i] > me ? s.hist[i] : 0;
-    const uint64_t at = drawn(u, all);
-    if (before <= at && at < before + s.hist[threadIdx.x])
-      put_token((int)~me, of_key((uint32_t)(s.sorted[threadIdx.x] >> 32)), all, sc, tokens, logprobs);
-    return;
-  }
-  const Keeps stays(choose_many(row, sc, how, g));
-  // sums of stretches of 64 units, one for each tile and wave, in the order of the ids
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  lds_barrier();
-  row.template each<4>([&](int j, int i, const u32x4& un) {
-    uint64_t sum = 0;
-#pragma unroll
-    for (int e = 0; e < R::E; ++e) {
-      const float x = from_bits<R::T>(lift<R::T>(un, e));
-      if (stays(x, i + e)) sum += weight(x, sc);
+  const int n = choose_few(row, t, sc, how, &all, s, g);
+  if ((int)threadIdx.x >= n) return;
+  // the running sum in the order of the ids, of which ~ makes the lower the greater
+  const uint32_t me = (uint32_t)s.sorted[threadIdx.x];
+  uint64_t before = 0;
+  for (int i = 0; i < n; ++i) before += (uint32_t)s.sorted[i] > me ? s.weights[i] : 0;
+  const uint64_t at = drawn(u, all);
+  if (before <= at && at < before + s.weights[threadIdx.x])
+    put_token((int)~me, of_key((uint32_t)(s.sorted[threadIdx.x] >> 32)), all, sc, tokens, logprobs);
+}
+
+template <class R>
+__global__ __launch_bounds__(R::LB) void k_sample_many(const void* logits, size_t ld, int V,
+                                                       LogitsChoice how, const float* uniforms,
+                                                       int* tokens, float* logprobs) {
+  __shared__ ManyLds s;
+  Group<R::W> g{s};
+  const float u = uniforms[blockIdx.x];
+  const R row(logits, ld, V);
+  for (int i = threadIdx.x; i < CELLS; i += R::LB) s.cells[i] = 0;
+  float ref = 0.f;
+  const float m = largest(row, how.c, how.top_p < 1, &ref, s, g);
+  if (!(m > -INFINITY)) return put_no_token(tokens, logprobs);
+  const Scale sc(m, how.c);
+  const Start st = start_many(row, ref, sc, how, s, g);
+  Kept k = st.plan.above;
+  uint64_t all, above;
+  const auto nothing = [](int, const u32x4&, const float(&)[R::E], const bool(&)[R::E]) {};
+  weigh(row, sc, st, true, &all, &above, s, g, nothing);
+  const int w = threadIdx.x >> 6;
+  if (st.plan.low < INFINITY) {
+    const int C = s.count;
+    if (decide(row, sc, how, st, all, above, C, &k, s, g) && st.least <= st.plan.above.key) {
+      const Keeps stays(k);
+      for (int i = threadIdx.x; i < C; i += R::LB) {
+        const float x = of_key((uint32_t)(s.list[i] >> 32));
+        const int id = (int)~(uint32_t)s.list[i];
+        const int cell = id / R::TILE * R::W + id % R::TILE / (64 * R::E);
+        if (stays(x, id)) atomicAdd((unsigned long long*)&s.cells[cell], weight(x, sc));
+      }
+    } else {
+      lds_barrier();
+      for (int i = threadIdx.x; i < CELLS; i += R::LB) s.cells[i] = 0;
+      lds_barrier();
+      const Start exact{{KEY_NINF + 1, 0x7FFFFFFF}, KEY_NINF + 1, {k, INFINITY}};
+      weigh(row, sc, exact, true, &all, &above, s, g, nothing);
     }
-    sum = wave_scan(sum, (uint64_t)0, Sum());
-    if (lane == 63) s.hist[j * R::W + w] = sum;
-  });
+  }
   lds_barrier();
   // the stretch that holds the place
-  const int n = (V + R::TILE - 1) / R::TILE * R::W;
-  const int per = (n + R::LB - 1) / R::LB;
-  uint64_t sum = 0;
-  for (int i = 0; i < per; ++i) {
-    const int q = threadIdx.x * per + i;
-    if (q < n) sum += s.hist[q];
-  }
+  constexpr int PER = CELLS / R::LB;
+  uint64_t h[PER], sum = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) sum += h[i] = s.cells[threadIdx.x * PER + i];
   uint64_t run = g.before(sum, &all);
   const uint64_t at = drawn(u, all);
   if (run <= at && at < run + sum) {
-    int q = threadIdx.x * per;
-    while (run + s.hist[q] <= at) run += s.hist[q++];
-    s.bin = q;
-    s.found[0] = run;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (run <= at && at < run + h[i]) {
+        s.bin = threadIdx.x * PER + i;
+        s.found[0] = run;
+      }
+      run += h[i];
+    }
   }
   lds_barrier();
   if (s.bin % R::W != w) return;
+  const Keeps stays(k);
   const int j = __builtin_amdgcn_readfirstlane(s.bin / R::W);
   const u32x4 un = row.load_tail(j);
   uint64_t ws[R::E];
@@ -743,47 +1179,60 @@ __global__ __launch_bounds__(R::LB) void k_sample(const void* logits, size_t ld,
   }
 }
 
-// The thread's sum of e^((x - m) / T), c = log2(e) / T, in 32 bits.
-template <class R>
-MSD_DEV float exp_sum(const R& row, float m, float c) {
-  float sum = 0.f;
+// The thread's largest logit, and its sum of e^((x - m) / T), c = log2(e) / T: a unit at a
+// time, the sum brought to a new largest one when that comes.
+struct Online {
+  float m = -INFINITY, sum = 0.f;
+};
+MSD_DEV float exp_of(float x, float m, float c) { return __builtin_amdgcn_exp2f((x - m) * c); }
+template <bool NO_NAN, class R>
+MSD_DEV Online online(const R& row, float c) {
+  Online o;
   row.template each<4>([&](int, int, const u32x4& u) {
+    float x[R::E], m = o.m;
 #pragma unroll
-    for (int e = 0; e < R::E; ++e)
-      sum += __builtin_amdgcn_exp2f((from_bits<R::T>(lift<R::T>(u, e)) - m) * c);
+    for (int e = 0; e < R::E; ++e) {
+      x[e] = from_bits<R::T>(lift<R::T>(u, e));
+      if (NO_NAN) x[e] = fmaxf(x[e], -INFINITY);
+      m = fmaxf(m, x[e]);
+    }
+    const float from = m > -INFINITY ? m : 0.f;  // (no inf - inf where all are masked)
+    float sum = o.sum * exp_of(o.m, from, c);
+#pragma unroll
+    for (int e = 0; e < R::E; ++e) sum += exp_of(x[e], from, c);
+    o = {m, sum};
   });
-  return sum;
+  return o;
+}
+// The same of the row, whose largest is m.
+template <int W>
+MSD_DEV double row_sum(const Online& o, float m, float c, Group<W>& g) {
+  return g.sum(o.sum == 0.f ? 0.0 : (double)(o.sum * exp_of(o.m, m, c)));
 }
 
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_top(const void* logits, size_t ld, int V, int n,
                                                float* values, int* ids, float* lse) {
-  __shared__ Lds s;
+  __shared__ FewLds s;
   Group<R::W> g{s};
   const R row(logits, ld, V);
-  const uint32_t mine = thread_max(row);
-  const float m = of_key(g.max(mine));
-  first_tokens(row, mine, n, g);
+  if (threadIdx.x == 0) s.count = 0;
+  constexpr float c = (float)M_LOG2E;
+  const Online on = online<true>(row, c);
+  const Tops t = tops(key_of(on.m), (n + R::W - 1) / R::W, g);
+  const float m = of_key(t.max);
+  if (lse) {
+    const double sum = row_sum(on, m, c, g);
+    if (threadIdx.x == 0)
+      lse[blockIdx.x] = fabsf(m) < INFINITY ? (float)((double)m + log(sum)) : m;
+  }
+  first_tokens(row, t, n, s, g);
   if ((int)threadIdx.x < n) {
     const size_t o = (size_t)blockIdx.x * n + threadIdx.x;
-    const uint64_t t = s.sorted[threadIdx.x];
-    values[o] = of_key((uint32_t)(t >> 32));
-    ids[o] = (int)~(uint32_t)t;
+    const uint64_t top = s.sorted[threadIdx.x];
+    values[o] = of_key((uint32_t)(top >> 32));
+    ids[o] = (int)~(uint32_t)top;
   }
-  if (!lse) return;
-  float l = m;
-  if (fabsf(m) < INFINITY) {
-    // (a NaN is no token)
-    float sum = 0.f;
-    row.template each<4>([&](int, int, const u32x4& u) {
-#pragma unroll
-      for (int e = 0; e < R::E; ++e)
-        sum += __builtin_amdgcn_exp2f(
-            fmaxf(from_bits<R::T>(lift<R::T>(u, e)) - m, -INFINITY) * (float)M_LOG2E);
-    });
-    l = (float)((double)m + log(g.sum((double)sum)));
-  }
-  if (threadIdx.x == 0) lse[blockIdx.x] = l;
 }
 
 // A row's teacher entry of this thread (id < 0: none).
@@ -793,78 +1242,109 @@ struct Entry {
   double lq, q;
 };
 
-// q = softmax(t / T) over the row's entries; all zero where none has a value above
-// -inf, NaN where one is NaN or +inf.
+// q = softmax(t / T) over the row's entries, the first k threads'; all zero where none has
+// a value above -inf, NaN where one is NaN or +inf.  Returns 1, 0 or NaN in these cases.
 template <int W>
-MSD_DEV void soften(Entry& e, double inv_t, Group<W>& g) {
+MSD_DEV double soften(Entry& e, int k, double inv_t, Group<W>& g) {
   const float top = of_key(g.max(key_of(e.value)));
-  const double d = ((double)e.value - (double)top) * inv_t;
-  const double w = e.value == -INFINITY ? 0 : exp(d);
+  double d = 0, w = 0;
+  if ((int)(threadIdx.x & ~63u) < k) {
+    d = ((double)e.value - (double)top) * inv_t;
+    w = e.value == -INFINITY ? 0 : exp(d);
+  }
   const double sum = g.sum(w);
   e.lq = e.q = 0;
   if (w != 0) {
     e.lq = d - log(sum);
     e.q = w / sum;
   }
+  return sum == 0 ? 0 : sum == sum ? 1 : sum;
 }
+
+// The entries as they meet the row's units: by the thread whose unit has their id, chained.
+struct Chains {
+  int id[LOGITS_TOP_MAX], next[LOGITS_TOP_MAX];
+  double q[LOGITS_TOP_MAX];
+  float gq[LOGITS_TOP_MAX];  // its part of the gradient
+  int head[1024];
+};
 
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_distill(const void* logits, size_t ld, int V,
                                                    LogitsTeacher t, float* loss, float* lse,
                                                    const float* grad, void* dx, size_t ldd) {
   __shared__ Lds s;
+  __shared__ Chains ch;
   Group<R::W> g{s};
   Entry e{-1, -INFINITY, 0, 0};
-  if ((int)threadIdx.x < t.k) {
-    const size_t o = (size_t)blockIdx.x * t.k + threadIdx.x;
+  const int lane_k = threadIdx.x;
+  if (lane_k < t.k) {
+    const size_t o = (size_t)blockIdx.x * t.k + lane_k;
     e.id = t.ids[o];
     if (e.id < 0 || e.id >= V) e.id = -1;
     if (e.id >= 0) e.value = t.values[o];
-    s.list[threadIdx.x] = (uint32_t)e.id;
   }
   const R row(logits, ld, V);
   const float zk = e.id >= 0 ? from_bits<R::T>(bits_at<R::T>(row.p, e.id)) : 0.f;
-  soften(e, t.inv_t, g);
+  const float gr = grad ? grad[blockIdx.x] : 0.f;
+  const double mass = soften(e, t.k, t.inv_t, g);
+  const float f = (float)(gr * t.inv_t * mass);
+  ch.head[threadIdx.x] = -1;
+  if (lane_k < t.k) {
+    ch.id[lane_k] = e.id;
+    ch.q[lane_k] = e.q;
+  }
+  lds_barrier();
+  if (dx && e.id >= 0) {
+    // the first entry of an id carries the others'
+    double q = 0;
+    bool first = true;
+    for (int i = 0; i < t.k; ++i) {
+      if (ch.id[i] != e.id) continue;
+      first = first && i >= lane_k;
+      q += ch.q[i];
+    }
+    if (first) {
+      ch.gq[lane_k] = (float)(f * q);
+      ch.next[lane_k] = atomicExch(&ch.head[e.id / R::E % R::LB], lane_k);
+    }
+  }
   const float c = (float)(t.inv_t * M_LOG2E);
-  // a NaN is passed over here and found again by the sum
-  const float m = of_key(g.max(thread_max(row)));
-  const double sum = g.sum((double)exp_sum(row, m, c));
-  const double dk = ((double)zk - (double)m) * t.inv_t;
-  const double l = g.sum(e.q != 0 ? e.q * (e.lq - (dk - log(sum))) : 0.0);
-  if (loss && threadIdx.x == 0) loss[blockIdx.x] = (float)l;
-  if (lse && threadIdx.x == 0) lse[blockIdx.x] = (float)(m * t.inv_t + log(sum));
-  if (!dx) return;
+  const Online on = online<false>(row, c);
   // the entries' logits are read before a gradient in their place is written
   asm volatile("" ::"v"(zk));
-  if ((int)threadIdx.x < t.k) s.hist[threadIdx.x] = (uint64_t)__double_as_longlong(e.q);
-  const double mass = g.sum(e.q);  // 1 (or NaN); 0 without entries
-  const double gr = mass == 0 ? 0 : grad[blockIdx.x] * t.inv_t * mass;
-  char* const o = static_cast<char*>(dx) + (size_t)blockIdx.x * ldd * Type<R::T>::SIZE;
-  if (mass == 0) {
-    const u32x4 none = 0u;
-    row.template each<4>([&](int, int i, const u32x4&) { row.store(o, i, none); });
-    return;
-  }
-  const float f = (float)(gr / sum);
-  row.template each<4>([&](int, int i, const u32x4& u) {
-    u32x4 y;
+  // (a NaN is passed over here and found again by the sum)
+  const float m = of_key(g.max(key_of(on.m)));
+  const double sum = row_sum(on, m, c, g);
+  if (dx) {
+    char* const o = static_cast<char*>(dx) + (size_t)blockIdx.x * ldd * Type<R::T>::SIZE;
+    const float fs = f / (float)sum;
+    const int head = ch.head[threadIdx.x];
+    row.template each<4>([&](int, int i, const u32x4& u) {
+      float y[R::E];
 #pragma unroll
-    for (int e = 0; e < R::E; ++e)
-      lower<R::T>(y, e,
-                  to_bits<R::T>(f * __builtin_amdgcn_exp2f(
-                                        (from_bits<R::T>(lift<R::T>(u, e)) - m) * c)));
-    row.store(o, i, y);
-  });
-  __syncthreads();
-  if (e.id < 0) return;
-  // the first entry of an id carries the others'
-  double q = 0;
-  for (int i = 0; i < t.k; ++i) {
-    if ((int)(uint32_t)s.list[i] != e.id) continue;
-    if (i < (int)threadIdx.x) return;
-    q += __longlong_as_double((long long)s.hist[i]);
+      for (int q = 0; q < R::E; ++q) {
+        y[q] = fs * exp_of(from_bits<R::T>(lift<R::T>(u, q)), m, c);
+        if (mass == 0) y[q] = 0.f;
+      }
+      for (int k = head; k >= 0; k = ch.next[k]) {
+        const int at = ch.id[k] - i;
+        const float gq = ch.gq[k];
+#pragma unroll
+        for (int q = 0; q < R::E; ++q) y[q] -= at == q ? gq : 0.f;
+      }
+      row.store(o, i, pack<R::T>(y));
+    });
   }
-  put_bits<R::T>(o, e.id, to_bits<R::T>((float)(gr * (exp(dk) / sum - q))));
+  if (!loss && !lse) return;
+  const bool mine = (int)(threadIdx.x & ~63u) < t.k;
+  double l = 0;
+  const double ls = mine ? log(sum) : 0;
+  if (mine && e.q != 0) l = e.q * (e.lq - (((double)zk - (double)m) * t.inv_t - ls));
+  l = g.sum(l);
+  if (threadIdx.x) return;
+  if (loss) loss[blockIdx.x] = (float)l;
+  if (lse) lse[blockIdx.x] = (float)(m * t.inv_t + ls);
 }
 
 }  // namespace
@@ -881,20 +1361,42 @@ void by_type(int type, F f) {
     f(std::integral_constant<int, MX_F16>());
 }
 
+template <class R>
+struct Tag {
+  using type = R;
+};
+
 // Rows of up to this many bytes take a workgroup of 256 threads.
 constexpr int SHORT_ROW = 256 * 8 * 16;
+
+template <class R>
+bool holds(int cols) {
+  return cols / R::TILE <= R::UNITS;
+}
+
+// Calls f with a row type for each way to hold a row of `cols`: 256 threads for a short
+// one; up to LONG tiles of 1024 threads in registers; or read from memory in every pass.
+template <int TYPE, int LONG, bool SHARE, class F>
+void by_row(int rows, int cols, F f) {
+  if (cols * Type<TYPE>::SIZE <= SHORT_ROW) return f(Tag<HeldRow<TYPE, 256, 8>>());
+  if constexpr (SHARE)
+    if (rows > 256 && holds<HeldRow<TYPE, 512, 16>>(cols)) return f(Tag<HeldRow<TYPE, 512, 16>>());
+  if (holds<HeldRow<TYPE, 1024, 8>>(cols)) return f(Tag<HeldRow<TYPE, 1024, 8>>());
+  if constexpr (LONG > 0)
+    if (holds<HeldRow<TYPE, 1024, LONG>>(cols)) return f(Tag<HeldRow<TYPE, 1024, LONG>>());
+  f(Tag<HeldRow<TYPE, 1024, 0>>());
+}
 
 }  // namespace
 
 void launch_logits_top(const void* x, int type, size_t ld, int rows, int cols, int k, float* values,
                        int* ids, float* lse, hipStream_t st) {
   if (rows <= 0) return;
-  by_type(type, [&](auto t_) {
-    constexpr int TYPE = decltype(t_)::value;
-    if (cols * Type<TYPE>::SIZE <= SHORT_ROW)
-      k_top<Row<TYPE, 256>><<<rows, 256, 0, st>>>(x, ld, cols, k, values, ids, lse);
-    else
-      k_top<Row<TYPE, 1024>><<<rows, 1024, 0, st>>>(x, ld, cols, k, values, ids, lse);
+  by_type(type, [&](auto t) {
+    by_row<t(), 19, true>(rows, cols, [&](auto r) {
+      using R = typename decltype(r)::type;
+      k_top<R><<<rows, R::LB, 0, st>>>(x, ld, cols, k, values, ids, lse);
+    });
   });
 }
 
@@ -902,13 +1404,18 @@ void launch_logits_sample(const void* x, int type, size_t ld, int rows, int cols
                           const LogitsChoice& how, const float* uniforms, int* tokens,
                           float* logprobs, hipStream_t st) {
   if (rows <= 0) return;
-  by_type(type, [&](auto t_) {
-    constexpr int TYPE = decltype(t_)::value;
-    if (cols * Type<TYPE>::SIZE <= SHORT_ROW)
-      k_sample<Row<TYPE, 256>><<<rows, 256, 0, st>>>(x, ld, cols, how, uniforms, tokens, logprobs);
+  const bool few = how.top_k > 0 && how.top_k <= LOGITS_TOP_MAX;
+  by_type(type, [&](auto t) {
+    if (few)
+      by_row<t(), 19, false>(rows, cols, [&](auto r) {
+        using R = typename decltype(r)::type;
+        k_sample_few<R><<<rows, R::LB, 0, st>>>(x, ld, cols, how, uniforms, tokens, logprobs);
+      });
     else
-      k_sample<Row<TYPE, 1024>>
-          <<<rows, 1024, 0, st>>>(x, ld, cols, how, uniforms, tokens, logprobs);
+      by_row<t(), 0, false>(rows, cols, [&](auto r) {
+        using R = typename decltype(r)::type;
+        k_sample_many<R><<<rows, R::LB, 0, st>>>(x, ld, cols, how, uniforms, tokens, logprobs);
+      });
   });
 }
 
@@ -916,34 +1423,30 @@ void launch_logits_filter(const void* x, int type, size_t ld, int rows, int cols
                           const LogitsChoice& how, void* out, size_t ldo, int* kept,
                           hipStream_t st) {
   if (rows <= 0) return;
-  by_type(type, [&](auto t_) {
-    constexpr int TYPE = decltype(t_)::value;
-    if (cols * Type<TYPE>::SIZE <= SHORT_ROW)
-      k_filter<Row<TYPE, 256>><<<rows, 256, 0, st>>>(x, ld, cols, how, out, ldo, kept);
+  const bool few = how.top_k > 0 && how.top_k <= LOGITS_TOP_MAX;
+  by_type(type, [&](auto t) {
+    if (few)
+      by_row<t(), 19, false>(rows, cols, [&](auto r) {
+        using R = typename decltype(r)::type;
+        k_filter_few<R><<<rows, R::LB, 0, st>>>(x, ld, cols, how, out, ldo, kept);
+      });
     else
-      k_filter<Row<TYPE, 1024>><<<rows, 1024, 0, st>>>(x, ld, cols, how, out, ldo, kept);
+      by_row<t(), 0, false>(rows, cols, [&](auto r) {
+        using R = typename decltype(r)::type;
+        k_filter_many<R><<<rows, R::LB, 0, st>>>(x, ld, cols, how, out, ldo, kept);
+      });
   });
 }
 
 void launch_logits_distill(const void* x, int type, size_t ld, int rows, int cols,
-                           const LogitsTeacher& t, float* loss, float* lse, const float* grad,
+                           const LogitsTeacher& t_, float* loss, float* lse, const float* grad,
                            void* dx, size_t ldd, hipStream_t st) {
   if (rows <= 0) return;
-  by_type(type, [&](auto t_) {
-    constexpr int TYPE = decltype(t_)::value;
-    const int tiles = cols / (1024 * Type<TYPE>::E);  // whole ones
-    if (cols * Type<TYPE>::SIZE <= SHORT_ROW)
-      k_distill<HeldRow<TYPE, 256, 8>>
-          <<<rows, 256, 0, st>>>(x, ld, cols, t, loss, lse, grad, dx, ldd);
-    else if (tiles <= 8)
-      k_distill<HeldRow<TYPE, 1024, 8>>
-          <<<rows, 1024, 0, st>>>(x, ld, cols, t, loss, lse, grad, dx, ldd);
-    else if (tiles <= 19)
-      k_distill<HeldRow<TYPE, 1024, 19>>
-          <<<rows, 1024, 0, st>>>(x, ld, cols, t, loss, lse, grad, dx, ldd);
-    else
-      k_distill<HeldRow<TYPE, 1024, 0>>
-          <<<rows, 1024, 0, st>>>(x, ld, cols, t, loss, lse, grad, dx, ldd);
+  by_type(type, [&](auto t) {
+    by_row<t(), 19, true>(rows, cols, [&](auto r) {
+      using R = typename decltype(r)::type;
+      k_distill<R><<<rows, R::LB, 0, st>>>(x, ld, cols, t_, loss, lse, grad, dx, ldd);
+    });
   });
 }
 

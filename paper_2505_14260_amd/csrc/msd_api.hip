@@ -2562,8 +2562,8 @@ int msd_logits_distill(const void* logits_d, int type, size_t ld, int rows, int 
   TRY(logits_float(logits_d, type, ld, rows, cols, &x));
   if (!teacher || teacher->k < 1 || teacher->k > LOGITS_TOP_MAX)
     return mx_fail(MSD_ERR_INVALID_ARG, "distill: wants a teacher of 1 .. 256 entries a row");
-  if (!(teacher->temperature >= 1e-6) || !std::isfinite(teacher->temperature))
-    return mx_fail(MSD_ERR_INVALID_ARG, "distill: temperature must be finite and 1e-6 at least");
+  if (!(teacher->temperature >= 1e-6 && teacher->temperature <= 1e6))
+    return mx_fail(MSD_ERR_INVALID_ARG, "distill: temperature must be 1e-6 .. 1e6");
   if (rows && ((!grad_d != !dlogits_d) || (!loss_d && !lse_d && !dlogits_d)))
     return mx_fail(MSD_ERR_INVALID_ARG,
                    "distill: wants an output, and the rows' weights with the gradient");

@@ -7,14 +7,18 @@ quotient of two sums, the larger at least 1, by twice that; the exponential is o
 2^-44 of itself at most, the quotient by twice that: (V + 4) 2^-44 covers them.
   log-probabilities: the same sum, and one rounding to float32.
 
-Sums of 32-bit weights e^-d (log-sum-exp, loss, gradient), d = (max - x) / T: the
-difference, its product with log2(e) / T and the constant are rounded (3 2^-24 of d at
-most), the exponential to 2^-23, a thread adds up to n = V / 64 of them one by one, and
-the rest is summed in 64 bits.  With D the mean of d under p the sum is off by
-  S = (3 D + 2 + n) 2^-24 relative;
-lse and loss by S (their logarithm is taken in 64 bits) and one rounding of the result;
-a p by S + (3 d + 2) 2^-24 of itself, and dx = g / T (p - q) by three more roundings of
-either term and half a step of the output type.
+Sums of 32-bit weights e^-d (log-sum-exp, loss, gradient), d = (max - x) / T.  A weight is
+the product of the exponentials by which a thread's largest logit rose since, of the last
+step to the row's, and its own: their arguments sum to d, each rounded with its difference
+and with log2(e) / T (3 2^-24 of d together); each exponential is off by 2^-23 and its
+product rounded (3 2^-24).  A thread of the 256 or 1024 of a row has units of 4 values or
+more: at most V / 1024 + 1 rises, the last step and its own exponential, so 3 (V / 1024 + 3)
+2^-24, and it adds its V / 256 + 8 values at most one by one; the rest is summed in 64
+bits.  With D the mean of d under p a sum is off by
+  S = (3 D + V / 64 + 18) 2^-24 relative
+at most; lse and loss by S (their logarithm is taken in 64 bits) and one rounding of the
+result; a p by S + (3 d + 2) 2^-24 of itself, and dx = g / T (p - q) by three more
+roundings of either term and half a step of the output type.
 """
 import numpy as np
 import pytest
@@ -78,7 +82,7 @@ def sum_error(x, temperature):
         d = (x.max() - x) / temperature
         p = np.exp(-d)
         D = np.where(p > 0, p * d, 0).sum() / p.sum()
-    return (3 * D + 2 + len(x) / 64) * U, d
+    return (3 * D + 18 + len(x) / 64) * U, d
 
 
 # --- top -----------------------------------------------------------------------------------

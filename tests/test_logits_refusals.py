@@ -61,7 +61,7 @@ def test_bad_logits(call, bad):
     (filter_, dict(out=None)), (filter_, dict(ldo=V - 1)), (filter_, dict(out=Y + 2)),
     (filter_, dict(kept=A + 3)),
     (distill, dict(k=0)), (distill, dict(k=257)), (distill, dict(ids=None)), (distill, dict(values=None)),
-    (distill, dict(T=0.0)), (distill, dict(T=9e-7)), (distill, dict(T=-1.0)), (distill, dict(T=float("inf"))),
+    (distill, dict(T=0.0)), (distill, dict(T=9e-7)), (distill, dict(T=1.1e6)), (distill, dict(T=-1.0)), (distill, dict(T=float("inf"))),
     (distill, dict(T=float("nan"))), (distill, dict(grad=None)), (distill, dict(dx=None)),
     (distill, dict(loss=None, lse=None, grad=None, dx=None)), (distill, dict(ldd=V - 1)),
     (distill, dict(dx=Y + 1))], ids=lambda v: v.__name__ if callable(v) else str(v))
