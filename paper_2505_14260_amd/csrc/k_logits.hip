@@ -98,23 +98,46 @@ MSD_DEV u32x4 pack(const float (&v)[Type<TYPE>::E]) {
   return u;
 }
 
-// A row of V logits over LB threads, in tiles of a unit of 16 bytes each: unit j of a
-// thread begins at element (j LB + thread) E; places past V hold -inf.
-template <int TYPE, int LB_>
+// A row of V logits over the W waves of LB threads, in units of 16 bytes a lane: 64 units,
+// a stretch, for a wave at a time.  A wave's stretches lie W apart (tiles of the whole
+// workgroup), or with RUNS one after the other, so that its sums are of neighbouring ids.
+// Places past V hold -inf.
+template <int TYPE, int LB_, bool RUNS = false>
 struct Row {
   static constexpr int T = TYPE, LB = LB_, E = Type<TYPE>::E, TILE = LB * E, W = LB / 64;
-  static constexpr bool HELD = false;
+  static constexpr int STRETCH = 64 * E;
   typedef typename Type<TYPE>::unit unit;
   const char* p;
   int V;
+  int at, full, part;  // the thread's first id; the wave's whole stretches, and any after them
 
   MSD_DEV Row(const void* base, size_t ld, int V_)
-      : p(static_cast<const char*>(base) + (size_t)blockIdx.x * ld * Type<TYPE>::SIZE), V(V_) {}
-  MSD_DEV int id(int j) const { return (j * LB + (int)threadIdx.x) * E; }
+      : p(static_cast<const char*>(base) + (size_t)blockIdx.x * ld * Type<TYPE>::SIZE), V(V_) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if constexpr (RUNS) {
+      const int n = per_wave(), first = wave * n;
+      full = min(max(V / STRETCH - first, 0), n);
+      part = full < n && (first + full) * STRETCH < V;
+      at = first * STRETCH + (threadIdx.x & 63) * E;
+    } else {
+      full = V / TILE;
+      part = V % TILE != 0;
+      at = threadIdx.x * E;
+    }
+  }
+  // The other order of the same row.
+  MSD_DEV explicit Row(const Row<TYPE, LB_, !RUNS>& o) : p(o.p), V(o.V) {
+    static_assert(!RUNS, "in tiles");
+    full = V / TILE;
+    part = V % TILE != 0;
+    at = threadIdx.x * E;
+  }
+  MSD_DEV int per_wave() const { return (V + TILE - 1) / TILE; }
+  MSD_DEV int id(int j) const { return at + j * (RUNS ? STRETCH : TILE); }
   MSD_DEV u32x4 load(int j) const {
     return *reinterpret_cast<const unit*>(p + (size_t)id(j) * Type<TYPE>::SIZE);
   }
-  // Of the last tile, where V may end inside a unit.
+  // One that V may end in.
   MSD_DEV u32x4 load_tail(int j) const {
     const int i = id(j);
     if (i + E <= V) return load(j);
@@ -124,15 +147,14 @@ struct Row {
       if (i + e < V) lower<TYPE>(u, e, bits_at<TYPE>(p, i + e));
     return u;
   }
-  // f(j, id, unit) for every tile in order, read from memory, the next AHEAD tiles
+  // f(j, id, unit) for every unit of the wave in order, read from memory, the next AHEAD
   // under way while f works on these.
   template <int AHEAD, class F>
   MSD_DEV void each(F f) const {
-    const int full = V / TILE;
     u32x4 next[AHEAD], last = Type<TYPE>::NINF;
 #pragma unroll
     for (int b = 0; b < AHEAD; ++b) next[b] = b < full ? load(b) : last;
-    if (V % TILE) last = load_tail(full);
+    if (part) last = load_tail(full);
     for (int j = 0; j < full; j += AHEAD) {
       u32x4 t[AHEAD];
 #pragma unroll
@@ -144,7 +166,7 @@ struct Row {
       for (int b = 0; b < AHEAD; ++b)
         if (j + b < full) f(j + b, id(j + b), t[b]);
     }
-    if (V % TILE) f(full, id(full), last);
+    if (part) f(full, id(full), last);
   }
   MSD_DEV void store(char* o, int i, const u32x4& u) const {
     if (i + E <= V) {
@@ -160,28 +182,24 @@ struct Row {
 // The same with up to U whole tiles and the last one in registers.
 template <int TYPE, int LB, int U>
 struct HeldRow : Row<TYPE, LB> {
-  typedef Row<TYPE, LB> Base;
-  static constexpr bool HELD = true;
   static constexpr int UNITS = U;
   mutable u32x4 r[U], last;
-  MSD_DEV HeldRow(const void* base, size_t ld, int V) : Base(base, ld, V) {
-    const int full = V / Base::TILE;
+  MSD_DEV HeldRow(const void* base, size_t ld, int V) : Row<TYPE, LB>(base, ld, V) {
 #pragma unroll
-    for (int j = 0; j < U; ++j) r[j] = j < full ? this->load(j) : u32x4(Type<TYPE>::NINF);
+    for (int j = 0; j < U; ++j) r[j] = j < this->full ? this->load(j) : u32x4(Type<TYPE>::NINF);
     last = Type<TYPE>::NINF;
-    if (V % Base::TILE) last = this->load_tail(full);
+    if (this->part) last = this->load_tail(this->full);
   }
   template <int AHEAD, class F>
   MSD_DEV void each(F f) const {
-    const int full = this->V / Base::TILE;
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       // so that no pass keeps its converted values for the next one
       asm("" : "+v"(r[j]));
-      if (j < full) f(j, this->id(j), r[j]);
+      if (j < this->full) f(j, this->id(j), r[j]);
     }
     asm("" : "+v"(last));
-    if (this->V % Base::TILE) f(full, this->id(full), last);
+    if (this->part) f(this->full, this->id(this->full), last);
   }
 };
 template <int TYPE, int LB>
@@ -218,7 +236,8 @@ struct Scale {
     return finite ? x : x == INFINITY ? 0.f : -INFINITY;
   }
 };
-MSD_DEV uint64_t weight_of(float x, const Scale& s) {
+// With 128 added, as a double: sums of n such bits are n times 128's more than the sum.
+MSD_DEV uint64_t bits_of(float x, const Scale& s) {
   const double t = fmax(((double)x - s.m64) * s.c, -64.0);  // (a NaN too)
   const double k = t + 0x1.8p52;                          // rounded in its last bits
   const double r = t - (k - 0x1.8p52);
@@ -234,9 +253,10 @@ MSD_DEV uint64_t weight_of(float x, const Scale& s) {
   q = fma(q, r, 1.0);
   const double w = __builtin_amdgcn_ldexp(q, (int)__double2loint(k));
   // the last bit of a double in [128, 256) is 2^-45
-  return (uint64_t)(__double_as_longlong(w + 128.0) - 0x4060000000000000ll);
+  return (uint64_t)__double_as_longlong(w + 128.0);
 }
-MSD_DEV uint64_t weight(float x, const Scale& s) { return weight_of(s(x), s); }
+constexpr uint64_t BITS_128 = 0x4060000000000000ull;
+MSD_DEV uint64_t weight(float x, const Scale& s) { return bits_of(s(x), s) - BITS_128; }
 
 // ------------------------------------------------------- waves and workgroups ----
 
@@ -444,22 +464,25 @@ MSD_DEV Kept shortest(const R& row, const Scale* sc, uint64_t want, uint64_t* hi
   if (sc) each = weight(of_key(prefix), *sc);
   const uint64_t n = (want + each - 1) / each;  // of the equal ones, at least 1
   if (n * each >= ties) return {prefix, row.V};
-  // the n-th of them in the order of their ids
+  // the n-th of them in the order of their ids, a tile at a time
+  const Row<R::T, R::LB> tiles(row);
+  const int end = (row.V + R::TILE - 1) / R::TILE;
   uint64_t seen = 0;
-  row.template each<1>([&](int, int i, const u32x4& u) {
-    if (seen >= n) return;
+  for (int j = 0; j < end && seen < n; ++j) {
+    const u32x4 u = tiles.load_tail(j);
+    const int i = tiles.id(j);
     int hits = 0;
 #pragma unroll
     for (int e = 0; e < R::E; ++e)
       hits += i + e < row.V && key_of(from_bits<R::T>(lift<R::T>(u, e))) == prefix;
     uint64_t before = seen + g.before(hits, &all);
     seen += all;
-    if (before >= n || before + hits < n) return;
+    if (before >= n || before + hits < n) continue;
 #pragma unroll
     for (int e = 0; e < R::E; ++e)
       if (i + e < row.V && key_of(from_bits<R::T>(lift<R::T>(u, e))) == prefix && ++before == n)
         s.bin = i + e;
-  });
+  }
   lds_barrier();
   return {prefix, s.bin};
 }
@@ -649,22 +672,25 @@ MSD_DEV int choose_few(const R& row, const Tops& t, const Scale& sc, const Logit
 // ------------------------------------------------- any number of tokens that stay ----
 
 // The pass that finds a row's largest counts its logits too, in COUNTS bins of T / 64
-// around one of them (`ref`, the largest of its first tile or of all), HEAD bins above
-// it.  With the counts and the weights of the bins' middles the border of top-p is known
-// to a bin or two.  The next pass computes the weights: those of all for their sum, those
-// that surely stay, and it lists a few thousand tokens around the estimate, among which
-// the border then has to lie.  Where it does not (rows of very many equal logits), the
-// border is found digit by digit.
+// around one of them (`ref`, the largest of its waves' first), HEAD bins above it, with
+// the sums of their places in the bins.  Weights at the means of the bins are off by
+// (1 / 64)^2 / 24 = 1e-5 at most, all nearly alike, so that they give the border of top-p
+// to a few tokens.  The next pass computes the weights: those of all for their sum, those
+// that surely stay, and it lists the tokens around the estimate, among which the border
+// then has to lie.  Where it does not (rows of very many equal logits), the border is
+// found digit by digit.
 constexpr int COUNTS = 4096, HEAD = 1024;
 constexpr double COUNTS_PER_T = 64;
+constexpr int PLACE_BITS = 40;              // of a bin's sum of places, in 2^-20
 constexpr int MANY = 4096;                  // the list, of up to
-constexpr int ABOVE = 1024, BELOW = 1536;   // so many before and after the border's bin
+constexpr int ABOVE = 64, BELOW = 128;      // so many before and after the border's bin
 constexpr int BORDER = 512;                 // of those that share the border's bin of the list
-constexpr int CELLS = LOGITS_MAX_COLS / 256;  // stretches of 64 units: tiles times waves
+constexpr int GROUP = 8;  // stretches of a wave that are summed together: a cell
+constexpr int CELLS = 256;  // a row's, 16 to a wave
 struct ManyLds : Lds {
   union {
     uint64_t hist[BINS];
-    uint32_t counts[COUNTS];
+    uint64_t counts[COUNTS];
   };
   uint64_t list[MANY];
   uint64_t few[BORDER], few_w[BORDER];
@@ -683,45 +709,33 @@ struct Bins {
 // The row's largest, and with `count` its counts.
 template <class R>
 MSD_DEV float largest(const R& row, double c, bool count, float* ref, ManyLds& s, Group<R::W>& g) {
-  const auto counted = [&](float x, const Bins& bins) {
-    const float b = bins.at(x);
-    if (b >= 0.f) atomicAdd(&s.counts[(int)fminf(b, (float)(COUNTS - 1))], 1u);
-  };
+  if (!count) return of_key(g.max(thread_max(row)));
+  for (int i = threadIdx.x; i < COUNTS; i += R::LB) s.counts[i] = 0;
   float m = -INFINITY;
-  if (count)
-    for (int i = threadIdx.x; i < COUNTS; i += R::LB) s.counts[i] = 0;
-  if constexpr (R::HELD) {
-    m = of_key(g.max(thread_max(row)));  // (its barrier: the counts are clear)
-    if (!count) return m;
-    const Bins bins(m, c);
-    row.template each<2>([&](int, int, const u32x4& u) {
-#pragma unroll
-      for (int e = 0; e < R::E; ++e) counted(from_bits<R::T>(lift<R::T>(u, e)), bins);
-    });
-    lds_barrier();
-    *ref = m;
-  } else {
-    if (!count) return of_key(g.max(thread_max(row)));
+  if (row.full || row.part) {
     const u32x4 first = row.load_tail(0);
 #pragma unroll
     for (int e = 0; e < R::E; ++e) m = fmaxf(m, from_bits<R::T>(lift<R::T>(first, e)));
-    *ref = of_key(g.max(key_of(m)));
-    const Bins bins(*ref, c);
-    row.template each<4>([&](int, int, const u32x4& u) {
-#pragma unroll
-      for (int e = 0; e < R::E; ++e) {
-        const float x = from_bits<R::T>(lift<R::T>(u, e));
-        m = fmaxf(m, x);
-        counted(x, bins);
-      }
-    });
-    m = of_key(g.max(key_of(m)));
   }
-  return m;
+  *ref = of_key(g.max(key_of(m)));  // (its barrier: the counts are clear)
+  const Bins bins(*ref, c);
+  row.template each<4>([&](int, int, const u32x4& u) {
+#pragma unroll
+    for (int e = 0; e < R::E; ++e) {
+      const float x = from_bits<R::T>(lift<R::T>(u, e));
+      m = fmaxf(m, x);
+      const float b = bins.at(x);
+      const float bin = fminf(floorf(b), (float)(COUNTS - 1));
+      if (b >= 0.f)
+        atomicAdd((unsigned long long*)&s.counts[(int)bin],
+                  1ull << PLACE_BITS | (uint32_t)(fminf(b - bin, 1.f) * 0x1p20f));
+    }
+  });
+  return of_key(g.max(key_of(m)));
 }
 
 // What is known before the weights: tokens that surely stay, and the least of the others
-// that may (+inf: none, the choice is exact).
+// that may (+inf: none, the choice is exact; else those that surely stay are all from a value on).
 struct Plan {
   Kept above;
   float low;
@@ -738,8 +752,10 @@ MSD_DEV Plan estimate(float ref, const Scale& sc, const LogitsChoice& how, uint3
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int b = COUNTS - 1 - (threadIdx.x * PER + i);
-    n[i] = s.counts[b];
-    sum += w[i] = n[i] * weight(fminf(bins.edge((float)b + 0.5f), sc.m), sc);
+    const uint64_t places = s.counts[b] & ((1ull << PLACE_BITS) - 1);
+    n[i] = (uint32_t)(s.counts[b] >> PLACE_BITS);
+    const float mean = (float)b + (float)places * 0x1p-20f / (float)n[i];  // (0 / 0: of none)
+    sum += w[i] = n[i] * weight(fminf(bins.edge(mean), sc.m), sc);
     count += n[i];
   }
   if (least > KEY_NINF + 1) {
@@ -852,7 +868,7 @@ struct Start {
 template <class R>
 MSD_DEV Start start_many(const R& row, float ref, const Scale& sc, const LogitsChoice& how,
                          ManyLds& s, Group<R::W>& g) {
-  const Row<R::T, R::LB>& mem = row;
+  const R& mem = row;
   constexpr int LAST = 0x7FFFFFFF;
   Start st{{KEY_NINF + 1, LAST}, KEY_NINF + 1, {{0xFF800000u, -1}, 3.402823466e38f}};
   if (how.min_d > -INFINITY) st.least = min_key(sc.m, how.min_d);
@@ -886,67 +902,78 @@ MSD_DEV Start start_many(const R& row, float ref, const Scale& sc, const LogitsC
   return st;
 }
 
-// The pass that computes the weights of a row: their sum, where the plan is not exact, and
-// that of the tokens that surely stay, also by stretches; the tokens that may stay are
-// listed.  f is called for each unit with its values and those that surely stay.
-template <class R, class F>
-MSD_DEV void weigh(const R& row, const Scale& sc, const Start& st, bool by_cell, uint64_t* all,
-                   uint64_t* above, ManyLds& s, Group<R::W>& g, F f) {
+// The pass that computes the weights of a row: the sums of all (with !EXACT) and of those
+// that surely stay, by cells too.  Units that hold tokens that only may stay are marked
+// and read again for the list, which they are few of.  f is called for each unit.
+template <bool EXACT, class R, class F>
+MSD_DEV void weigh(const R& row, const Scale& sc, const Start& st, uint64_t* all, uint64_t* above,
+                   ManyLds& s, Group<R::W>& g, F f) {
   const Keeps stays(st.plan.above), within(st.limit);
   const float low = st.plan.low;
-  const bool exact = low == INFINITY, limited = st.limit.key > KEY_NINF + 1;
+  const bool limited = !EXACT && st.limit.key > KEY_NINF + 1;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  uint64_t sum_all = 0, sum_above = 0;
+  uint64_t sum_all = 0, sum_above = 0, cell = 0, marked = 0;
+  const int pairs = row.per_wave() > 64;  // a mark is of two units
+  const auto close = [&](int j) {
+    const uint64_t t = wave_scan(cell, (uint64_t)0, Sum());
+    if (lane == 63) s.cells[wave * (CELLS / 16) + j / GROUP] = t;
+    sum_above += cell;
+    cell = 0;
+  };
   row.template each<2>([&](int j, int i, const u32x4& u) {
     float x[R::E];
-    bool in[R::E], any = false;
-    int listed = 0;
+    bool in[R::E], any = false, may = false;
 #pragma unroll
-    for (int e = 0; e < R::E; ++e) {
-      x[e] = from_bits<R::T>(lift<R::T>(u, e));
-      if (limited && !within(x[e], i + e)) x[e] = -INFINITY;
-      any |= in[e] = stays(x[e], i + e);
-      listed += x[e] >= low && !in[e];
-    }
-    if (listed) {
-      int at = atomicAdd(&s.count, listed);
+    for (int e = 0; e < R::E; ++e) x[e] = from_bits<R::T>(lift<R::T>(u, e));
+    if (limited) {
 #pragma unroll
       for (int e = 0; e < R::E; ++e)
-        if (x[e] >= low && !in[e]) {
-          if (at < MANY) s.list[at] = place_of(key_of(x[e]), i + e);
-          ++at;
-        }
+        if (!within(x[e], i + e)) x[e] = -INFINITY;
     }
-    const bool some = __any(any);
-    if (!exact || some) {
+#pragma unroll
+    for (int e = 0; e < R::E; ++e) {
+      in[e] = EXACT ? stays(x[e], i + e) : x[e] >= stays.x;
+      any |= in[e];
+      if (!EXACT) may |= x[e] >= low && !in[e];
+    }
+    if (!EXACT) marked |= (uint64_t)may << (j >> pairs);
+    if (!EXACT || __any(any)) {
       float z[R::E];
 #pragma unroll
       for (int e = 0; e < R::E; ++e) z[e] = x[e];
-      if (!sc.finite) {
+      if (EXACT && !sc.finite) {
 #pragma unroll
         for (int e = 0; e < R::E; ++e) z[e] = sc(x[e]);
       }
-      uint64_t a = 0;
 #pragma unroll
       for (int h = 0; h < R::E; h += 4) {  // in fours: registers for their arithmetic
         if (h) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int e = h; e < h + 4; ++e) {
-          const uint64_t w = weight_of(z[e], sc);
-          sum_all += w;
-          a += in[e] ? w : 0;
+          const uint64_t w = bits_of(z[e], sc);
+          if (!EXACT) sum_all += w;
+          cell += in[e] ? w : BITS_128;
         }
       }
-      sum_above += a;
-      if (by_cell && some) {
-        a = wave_scan(a, (uint64_t)0, Sum());
-        if (lane == 63) s.cells[j * R::W + wave] = a;
-      }
+      cell -= R::E * BITS_128;
+      if (!EXACT) sum_all -= R::E * BITS_128;
     }
+    if (j % GROUP == GROUP - 1) close(j);
     f(i, u, x, in);
   });
-  *all = exact ? 0 : g.sum(sum_all);
-  *above = g.sum(sum_above);  // (its barrier: the list is whole)
+  const int n = row.full + row.part;
+  if (n % GROUP) close(n - 1);
+  if (!EXACT) {
+    for (; marked; marked &= marked - 1) {
+      const int j0 = (__ffsll((unsigned long long)marked) - 1) << pairs;
+      for (int j = j0; j <= j0 + pairs && j < row.full + row.part; ++j)
+        append(row, row.id(j), row.load_tail(j), s.list, MANY, s, [&](float v, int id) {
+          return v >= low && !(v >= stays.x) && (!limited || within(v, id));
+        });
+    }
+    *all = g.sum(sum_all);
+  }
+  *above = g.sum(sum_above);  // (its barrier: the list and the cells are whole)
 }
 
 // The last token that stays, after a plan's weights; false where it had to be looked for
@@ -954,12 +981,11 @@ MSD_DEV void weigh(const R& row, const Scale& sc, const Start& st, bool by_cell,
 template <class R>
 MSD_DEV bool decide(const R& row, const Scale& sc, const LogitsChoice& how, const Start& st,
                     uint64_t all, uint64_t above, int C, Kept* k, ManyLds& s, Group<R::W>& g) {
-  const Row<R::T, R::LB>& mem = row;
   uint64_t want = (uint64_t)ceil((double)all * how.top_p);
   want = want < 1 ? 1 : want > all ? all : want;
   const bool found = C <= MANY && want > above &&
                      border<R::LB>(s, C, st.plan, want - above, sc, k, g);
-  if (!found) *k = shortest(mem, &sc, want, s.hist, g);
+  if (!found) *k = shortest(row, &sc, want, s.hist, g);
   if (st.least > k->key) *k = {st.least, 0x7FFFFFFF};
   return found;
 }
@@ -1022,12 +1048,12 @@ __global__ __launch_bounds__(R::LB) void k_filter_many(const void* logits, size_
     const Start st = start_many(row, ref, sc, how, s, g);
     k = st.plan.above;
     if (st.plan.low < INFINITY) {
-      // the pass over a row in memory writes as well, but for one that may have to be
-      // read again
-      const bool write = !R::HELD && out != logits;
+      // the pass writes as well, but in place, where the row may have to be read again
+      const bool write = out != logits;
       uint64_t all, above;
       uint32_t n = 0;
-      weigh(row, sc, st, false, &all, &above, s, g,
+      weigh<false>(
+            row, sc, st, &all, &above, s, g,
             [&](int i, const u32x4& u, const float(&x)[R::E], const bool(&in)[R::E]) {
               if (!write) return;
               u32x4 y = u;
@@ -1119,63 +1145,62 @@ __global__ __launch_bounds__(R::LB) void k_sample_many(const void* logits, size_
   Kept k = st.plan.above;
   uint64_t all, above;
   const auto nothing = [](int, const u32x4&, const float(&)[R::E], const bool(&)[R::E]) {};
-  weigh(row, sc, st, true, &all, &above, s, g, nothing);
   const int w = threadIdx.x >> 6;
-  if (st.plan.low < INFINITY) {
+  bool exact = st.plan.low == INFINITY;
+  if (!exact) {
+    weigh<false>(row, sc, st, &all, &above, s, g, nothing);
     const int C = s.count;
     if (decide(row, sc, how, st, all, above, C, &k, s, g) && st.least <= st.plan.above.key) {
       const Keeps stays(k);
       for (int i = threadIdx.x; i < C; i += R::LB) {
         const float x = of_key((uint32_t)(s.list[i] >> 32));
         const int id = (int)~(uint32_t)s.list[i];
-        const int cell = id / R::TILE * R::W + id % R::TILE / (64 * R::E);
+        const int q = id / R::STRETCH, wave = q / row.per_wave();
+        const int cell = wave * (CELLS / 16) + (q - wave * row.per_wave()) / GROUP;
         if (stays(x, id)) atomicAdd((unsigned long long*)&s.cells[cell], weight(x, sc));
       }
     } else {
-      lds_barrier();
-      for (int i = threadIdx.x; i < CELLS; i += R::LB) s.cells[i] = 0;
-      lds_barrier();
-      const Start exact{{KEY_NINF + 1, 0x7FFFFFFF}, KEY_NINF + 1, {k, INFINITY}};
-      weigh(row, sc, exact, true, &all, &above, s, g, nothing);
+      exact = true;
     }
+    lds_barrier();
   }
-  lds_barrier();
-  // the stretch that holds the place
-  constexpr int PER = CELLS / R::LB;
-  uint64_t h[PER], sum = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) sum += h[i] = s.cells[threadIdx.x * PER + i];
-  uint64_t run = g.before(sum, &all);
+  if (exact) {
+    for (int i = threadIdx.x; i < CELLS; i += R::LB) s.cells[i] = 0;
+    lds_barrier();
+    const Start chosen{{KEY_NINF + 1, 0x7FFFFFFF}, KEY_NINF + 1, {k, INFINITY}};
+    weigh<true>(row, sc, chosen, &all, &above, s, g, nothing);
+  }
+  // the cell that holds the place
+  const uint64_t h = (int)threadIdx.x < CELLS ? s.cells[threadIdx.x] : 0;
+  uint64_t run = g.before(h, &all);
   const uint64_t at = drawn(u, all);
-  if (run <= at && at < run + sum) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      if (run <= at && at < run + h[i]) {
-        s.bin = threadIdx.x * PER + i;
-        s.found[0] = run;
-      }
-      run += h[i];
-    }
+  if (run <= at && at < run + h) {
+    s.bin = threadIdx.x;
+    s.found[0] = run;
   }
   lds_barrier();
-  if (s.bin % R::W != w) return;
+  if (s.bin / (CELLS / 16) != w) return;
   const Keeps stays(k);
-  const int j = __builtin_amdgcn_readfirstlane(s.bin / R::W);
-  const u32x4 un = row.load_tail(j);
-  uint64_t ws[R::E];
-  sum = 0;
+  run = s.found[0];
+  const int from = __builtin_amdgcn_readfirstlane(s.bin % (CELLS / 16) * GROUP);
+  for (int j = from; j < from + GROUP && run <= at; ++j) {
+    const u32x4 un = row.load_tail(j);
+    uint64_t ws[R::E], sum = 0;
 #pragma unroll
-  for (int e = 0; e < R::E; ++e) {
-    const float x = from_bits<R::T>(lift<R::T>(un, e));
-    ws[e] = stays(x, row.id(j) + e) ? weight(x, sc) : 0;
-    sum += ws[e];
-  }
-  run = s.found[0] + wave_scan(sum, (uint64_t)0, Sum()) - sum;
+    for (int e = 0; e < R::E; ++e) {
+      const float x = from_bits<R::T>(lift<R::T>(un, e));
+      ws[e] = stays(x, row.id(j) + e) ? weight(x, sc) : 0;
+      sum += ws[e];
+    }
+    const uint64_t in = wave_scan(sum, (uint64_t)0, Sum());
+    uint64_t before = run + in - sum;
 #pragma unroll
-  for (int e = 0; e < R::E; ++e) {
-    if (run <= at && at < run + ws[e])
-      put_token(row.id(j) + e, from_bits<R::T>(lift<R::T>(un, e)), all, sc, tokens, logprobs);
-    run += ws[e];
+    for (int e = 0; e < R::E; ++e) {
+      if (before <= at && at < before + ws[e])
+        put_token(row.id(j) + e, from_bits<R::T>(lift<R::T>(un, e)), all, sc, tokens, logprobs);
+      before += ws[e];
+    }
+    run += __shfl((unsigned long long)in, 63);
   }
 }
 
@@ -1387,13 +1412,23 @@ void by_row(int rows, int cols, F f) {
   f(Tag<HeldRow<TYPE, 1024, 0>>());
 }
 
+template <int TYPE, class F>
+void by_runs(int rows, int cols, F f) {
+  if (cols * Type<TYPE>::SIZE <= SHORT_ROW)
+    f(Tag<Row<TYPE, 256, true>>());
+  else if (rows > 256)
+    f(Tag<Row<TYPE, 512, true>>());
+  else
+    f(Tag<Row<TYPE, 1024, true>>());
+}
+
 }  // namespace
 
 void launch_logits_top(const void* x, int type, size_t ld, int rows, int cols, int k, float* values,
                        int* ids, float* lse, hipStream_t st) {
   if (rows <= 0) return;
   by_type(type, [&](auto t) {
-    by_row<t(), 19, true>(rows, cols, [&](auto r) {
+    by_row<t(), 18, true>(rows, cols, [&](auto r) {
       using R = typename decltype(r)::type;
       k_top<R><<<rows, R::LB, 0, st>>>(x, ld, cols, k, values, ids, lse);
     });
@@ -1407,12 +1442,12 @@ void launch_logits_sample(const void* x, int type, size_t ld, int rows, int cols
   const bool few = how.top_k > 0 && how.top_k <= LOGITS_TOP_MAX;
   by_type(type, [&](auto t) {
     if (few)
-      by_row<t(), 19, false>(rows, cols, [&](auto r) {
+      by_row<t(), 18, false>(rows, cols, [&](auto r) {
         using R = typename decltype(r)::type;
         k_sample_few<R><<<rows, R::LB, 0, st>>>(x, ld, cols, how, uniforms, tokens, logprobs);
       });
     else
-      by_row<t(), 0, false>(rows, cols, [&](auto r) {
+      by_runs<t()>(rows, cols, [&](auto r) {
         using R = typename decltype(r)::type;
         k_sample_many<R><<<rows, R::LB, 0, st>>>(x, ld, cols, how, uniforms, tokens, logprobs);
       });
@@ -1426,12 +1461,12 @@ void launch_logits_filter(const void* x, int type, size_t ld, int rows, int cols
   const bool few = how.top_k > 0 && how.top_k <= LOGITS_TOP_MAX;
   by_type(type, [&](auto t) {
     if (few)
-      by_row<t(), 19, false>(rows, cols, [&](auto r) {
+      by_row<t(), 18, false>(rows, cols, [&](auto r) {
         using R = typename decltype(r)::type;
         k_filter_few<R><<<rows, R::LB, 0, st>>>(x, ld, cols, how, out, ldo, kept);
       });
     else
-      by_row<t(), 0, false>(rows, cols, [&](auto r) {
+      by_runs<t()>(rows, cols, [&](auto r) {
         using R = typename decltype(r)::type;
         k_filter_many<R><<<rows, R::LB, 0, st>>>(x, ld, cols, how, out, ldo, kept);
       });
@@ -1443,7 +1478,7 @@ void launch_logits_distill(const void* x, int type, size_t ld, int rows, int col
                            void* dx, size_t ldd, hipStream_t st) {
   if (rows <= 0) return;
   by_type(type, [&](auto t) {
-    by_row<t(), 19, true>(rows, cols, [&](auto r) {
+    by_row<t(), 18, true>(rows, cols, [&](auto r) {
       using R = typename decltype(r)::type;
       k_distill<R><<<rows, R::LB, 0, st>>>(x, ld, cols, t_, loss, lse, grad, dx, ldd);
     });
