@@ -170,7 +170,7 @@ struct Row {
   }
   MSD_DEV void store(char* o, int i, const u32x4& u) const {
     if (i + E <= V) {
-      *reinterpret_cast<unit*>(o + (size_t)i * Type<TYPE>::SIZE) = u;
+      __builtin_nontemporal_store(u, reinterpret_cast<unit*>(o + (size_t)i * Type<TYPE>::SIZE));
     } else {
 #pragma unroll
       for (int e = 0; e < E; ++e)
@@ -205,6 +205,40 @@ struct HeldRow : Row<TYPE, LB> {
 template <int TYPE, int LB>
 struct HeldRow<TYPE, LB, 0> : Row<TYPE, LB> {  // too long for that
   using Row<TYPE, LB>::Row;
+};
+
+// A row that is read once, of up to U whole tiles, AHEAD of them under way at a time, whose
+// units' largest stay in registers: they tell which few units to read again.
+template <int TYPE, int LB, int U, int AHEAD>
+struct ToppedRow : Row<TYPE, LB> {
+  using Row<TYPE, LB>::Row;
+  static constexpr int UNITS = U;
+  float top[U + 1];
+  // m = f(unit) for every unit in order, m its largest.
+  template <class F>
+  MSD_DEV void read(F f) {
+    u32x4 next[AHEAD], last = Type<TYPE>::NINF;
+#pragma unroll
+    for (int b = 0; b < AHEAD; ++b) next[b] = b < this->full ? this->load(b) : last;
+    if (this->part) last = this->load_tail(this->full);
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      top[j] = -INFINITY;
+      if (j < this->full) {
+        const u32x4 t = next[j % AHEAD];
+        if (j + AHEAD < this->full) next[j % AHEAD] = this->load(j + AHEAD);
+        top[j] = f(t);
+      }
+    }
+    top[U] = this->part ? f(last) : -INFINITY;
+  }
+  // The units that reach x.
+  MSD_DEV uint64_t reach(float x) const {
+    uint64_t m = this->part && top[U] >= x ? 1ull << this->full : 0;
+#pragma unroll
+    for (int j = 0; j < U; ++j) m |= (uint64_t)(top[j] >= x) << j;
+    return m;
+  }
 };
 
 // ----------------------------------------------------------- keys and weights ----
@@ -606,20 +640,24 @@ MSD_DEV void rank(FewLds& s, int C, int n, float m, float floor, Group<LB / 64>&
   lds_barrier();
 }
 
-// The first n (at most LOGITS_TOP_MAX and V) tokens of the row in order, in s.sorted:
-// those that reach a bound that n at least do, ranked.
+// A unit's largest.
 template <class R>
-MSD_DEV void first_tokens(const R& row, const Tops& t, int n, FewLds& s, Group<R::W>& g) {
+MSD_DEV float unit_max(const u32x4& u) {
+  float m = -INFINITY;
+#pragma unroll
+  for (int e = 0; e < R::E; ++e) m = fmaxf(m, from_bits<R::T>(lift<R::T>(u, e)));
+  return m;
+}
+
+// The first n (at most LOGITS_TOP_MAX and V) tokens of the row in order, in s.sorted:
+// those that reach a bound that n at least do, ranked.  reach(x): the thread's units with
+// one that reaches x, a bit each; they are few, and read again.
+template <class R, class F>
+MSD_DEV void first_tokens(const R& row, const Tops& t, int n, FewLds& s, Group<R::W>& g, F reach) {
   const bool all = t.floor <= KEY_NINF;
   const float at_least = all ? -INFINITY : of_key(t.floor);
   const Row<R::T, R::LB>& mem = row;
-  uint64_t units = 0;  // of the thread's, those with one: few, and read again
-  row.template each<4>([&](int j, int, const u32x4& u) {
-    float m = -INFINITY;
-#pragma unroll
-    for (int e = 0; e < R::E; ++e) m = fmaxf(m, from_bits<R::T>(lift<R::T>(u, e)));
-    units |= (uint64_t)(m >= at_least) << j;
-  });
+  uint64_t units = reach(at_least);
   for (; units; units &= units - 1) {
     const int j = __ffsll((unsigned long long)units) - 1;
     append(mem, mem.id(j), mem.load_tail(j), s.list, FEW, s,
@@ -644,11 +682,11 @@ MSD_DEV void first_tokens(const R& row, const Tops& t, int n, FewLds& s, Group<R
 
 // The tokens that stay of a few at most (0 < top_k <= LOGITS_TOP_MAX): their number, in
 // order in s.sorted, with their weights in s.weights and *all their sum.
-template <class R>
+template <class R, class F>
 MSD_DEV int choose_few(const R& row, const Tops& t, const Scale& sc, const LogitsChoice& how,
-                       uint64_t* all, FewLds& s, Group<R::W>& g) {
+                       uint64_t* all, FewLds& s, Group<R::W>& g, F reach) {
   const int n = min(how.top_k, row.V);
-  first_tokens(row, t, n, s, g);
+  first_tokens(row, t, n, s, g, reach);
   uint32_t key = 0;
   uint64_t w = 0;
   if ((int)threadIdx.x < n) {
@@ -682,8 +720,7 @@ MSD_DEV int choose_few(const R& row, const Tops& t, const Scale& sc, const Logit
 constexpr int COUNTS = 4096, HEAD = 1024;
 constexpr double COUNTS_PER_T = 64;
 constexpr int PLACE_BITS = 40;              // of a bin's sum of places, in 2^-20
-constexpr int MANY = 4096;                  // the list, of up to
-constexpr int ABOVE = 64, BELOW = 128;      // so many before and after the border's bin
+constexpr int MANY = 4096;                  // the list: the border's bin and those beside it
 constexpr int BORDER = 512;                 // of those that share the border's bin of the list
 constexpr int GROUP = 8;  // stretches of a wave that are summed together: a cell
 constexpr int CELLS = 256;  // a row's, 16 to a wave
@@ -695,7 +732,6 @@ struct ManyLds : Lds {
   uint64_t list[MANY];
   uint64_t few[BORDER], few_w[BORDER];
   uint64_t cells[CELLS];
-  int low, high;
 };
 
 struct Bins {
@@ -747,8 +783,8 @@ MSD_DEV Plan estimate(float ref, const Scale& sc, const LogitsChoice& how, uint3
                       ManyLds& s, Group<R::W>& g) {
   constexpr int PER = COUNTS / R::LB;
   const Bins bins(ref, sc.c);
-  uint32_t n[PER], count = 0;
-  uint64_t w[PER], sum = 0, all, tokens;
+  uint32_t n[PER];
+  uint64_t w[PER], sum = 0, all;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int b = COUNTS - 1 - (threadIdx.x * PER + i);
@@ -756,7 +792,6 @@ MSD_DEV Plan estimate(float ref, const Scale& sc, const LogitsChoice& how, uint3
     n[i] = (uint32_t)(s.counts[b] >> PLACE_BITS);
     const float mean = (float)b + (float)places * 0x1p-20f / (float)n[i];  // (0 / 0: of none)
     sum += w[i] = n[i] * weight(fminf(bins.edge(mean), sc.m), sc);
-    count += n[i];
   }
   if (least > KEY_NINF + 1) {
     // Does min_p end before top_p for certain?  Weights at the bins' edges, a hundredth
@@ -775,41 +810,28 @@ MSD_DEV Plan estimate(float ref, const Scale& sc, const LogitsChoice& how, uint3
       return {{least, 0x7FFFFFFF}, INFINITY};
   }
   uint64_t run = g.before(sum, &all);
-  uint32_t seen = (uint32_t)g.before(count, &tokens);
   const uint64_t want = (uint64_t)((double)all * how.top_p);
-  if (threadIdx.x == 0) {
-    s.bin = COUNTS - 1;
-    s.count = 0;
-  }
-  lds_barrier();
   if (run <= want && want < run + sum) {
-    uint32_t c = seen;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       if (run <= want && want < run + w[i]) {
         s.bin = COUNTS - 1 - (threadIdx.x * PER + i);
-        s.count = (int)c;
+        s.count = (int)n[i];
+        s.found[0] = (uint64_t)((double)(want - run) / (double)w[i] * 0x1p20);
       }
       run += w[i];
-      c += n[i];
     }
   }
   lds_barrier();
-  const int bin = s.bin, before = s.count;
-  if (threadIdx.x == 0) s.low = s.high = bin;
-  lds_barrier();
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int b = COUNTS - 1 - (threadIdx.x * PER + i);
-    if (b >= bin && (int)seen >= before - ABOVE) atomicMax(&s.high, b);
-    if (b <= bin && (int)(seen + n[i]) <= before + BELOW) atomicMin(&s.low, b);
-    seen += n[i];
-  }
-  if (threadIdx.x == 0) s.count = 0;
-  lds_barrier();
-  const float high = bins.edge((float)(s.high + 1));
-  Plan p{{0xFF800000u, -1}, bins.edge((float)s.low)};
-  if (s.high < COUNTS - 1 && high < sc.m) p.above = {key_of(high), 0x7FFFFFFF};
+  // Around its place in the bin if the bin's tokens lay evenly: a few of their standard
+  // deviations (of n in order, 1 / (2 sqrt(n)) at most), and no less than the bins beside
+  // it where they are few.
+  const float tokens = (float)s.count, down = (float)s.found[0] * 0x1p-20f;
+  const float around = tokens > 100.f ? 0.1f + 3.f * rsqrtf(tokens) : 1.5f;
+  const float at = (float)(s.bin + 1) - down;
+  const float high = bins.edge(at + around);
+  Plan p{{0xFF800000u, -1}, bins.edge(at - around)};
+  if (at + around < (float)COUNTS && high < sc.m) p.above = {key_of(high), 0x7FFFFFFF};
   return p;
 }
 
@@ -1024,7 +1046,13 @@ __global__ __launch_bounds__(R::LB) void k_filter_few(const void* logits, size_t
   int n = 0;
   if (t.max > KEY_NINF) {
     uint64_t all;
-    n = choose_few(row, t, Scale(of_key(t.max), how.c), how, &all, s, g);
+    n = choose_few(row, t, Scale(of_key(t.max), how.c), how, &all, s, g, [&](float x) {
+      uint64_t units = 0;
+      row.template each<4>([&](int j, int, const u32x4& u) {
+        units |= (uint64_t)(unit_max<R>(u) >= x) << j;
+      });
+      return units;
+    });
     const uint64_t last = s.sorted[n - 1];
     k = {(uint32_t)(last >> 32), (int)~(uint32_t)last};
   }
@@ -1111,13 +1139,19 @@ __global__ __launch_bounds__(R::LB) void k_sample_few(const void* logits, size_t
   __shared__ FewLds s;
   Group<R::W> g{s};
   const float u = uniforms[blockIdx.x];
-  const R row(logits, ld, V);
+  R row(logits, ld, V);
   if (threadIdx.x == 0) s.count = 0;
-  const Tops t = tops(thread_max(row), (min(how.top_k, V) + R::W - 1) / R::W, g);
+  float mine = -INFINITY;
+  row.read([&](const u32x4& un) {
+    const float m = unit_max<R>(un);
+    mine = fmaxf(mine, m);
+    return m;
+  });
+  const Tops t = tops(key_of(mine), (min(how.top_k, V) + R::W - 1) / R::W, g);
   if (t.max <= KEY_NINF) return put_no_token(tokens, logprobs);
   const Scale sc(of_key(t.max), how.c);
   uint64_t all;
-  const int n = choose_few(row, t, sc, how, &all, s, g);
+  const int n = choose_few(row, t, sc, how, &all, s, g, [&](float x) { return row.reach(x); });
   if ((int)threadIdx.x >= n) return;
   // the running sum in the order of the ids, of which ~ makes the lower the greater
   const uint32_t me = (uint32_t)s.sorted[threadIdx.x];
@@ -1210,24 +1244,23 @@ struct Online {
   float m = -INFINITY, sum = 0.f;
 };
 MSD_DEV float exp_of(float x, float m, float c) { return __builtin_amdgcn_exp2f((x - m) * c); }
+// Another unit; its largest.
 template <bool NO_NAN, class R>
-MSD_DEV Online online(const R& row, float c) {
-  Online o;
-  row.template each<4>([&](int, int, const u32x4& u) {
-    float x[R::E], m = o.m;
+MSD_DEV float add_unit(Online& o, const u32x4& u, float c) {
+  float x[R::E], top = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < R::E; ++e) {
-      x[e] = from_bits<R::T>(lift<R::T>(u, e));
-      if (NO_NAN) x[e] = fmaxf(x[e], -INFINITY);
-      m = fmaxf(m, x[e]);
-    }
-    const float from = m > -INFINITY ? m : 0.f;  // (no inf - inf where all are masked)
-    float sum = o.sum * exp_of(o.m, from, c);
+  for (int e = 0; e < R::E; ++e) {
+    x[e] = from_bits<R::T>(lift<R::T>(u, e));
+    if (NO_NAN) x[e] = fmaxf(x[e], -INFINITY);
+    top = fmaxf(top, x[e]);
+  }
+  const float m = fmaxf(o.m, top);
+  const float from = m > -INFINITY ? m : 0.f;  // (no inf - inf where all are masked)
+  float sum = o.sum * exp_of(o.m, from, c);
 #pragma unroll
-    for (int e = 0; e < R::E; ++e) sum += exp_of(x[e], from, c);
-    o = {m, sum};
-  });
-  return o;
+  for (int e = 0; e < R::E; ++e) sum += exp_of(x[e], from, c);
+  o = {m, sum};
+  return top;
 }
 // The same of the row, whose largest is m.
 template <int W>
@@ -1240,10 +1273,11 @@ __global__ __launch_bounds__(R::LB) void k_top(const void* logits, size_t ld, in
                                                float* values, int* ids, float* lse) {
   __shared__ FewLds s;
   Group<R::W> g{s};
-  const R row(logits, ld, V);
+  R row(logits, ld, V);
   if (threadIdx.x == 0) s.count = 0;
   constexpr float c = (float)M_LOG2E;
-  const Online on = online<true>(row, c);
+  Online on;
+  row.read([&](const u32x4& u) { return add_unit<true, R>(on, u, c); });
   const Tops t = tops(key_of(on.m), (n + R::W - 1) / R::W, g);
   const float m = of_key(t.max);
   if (lse) {
@@ -1251,7 +1285,7 @@ __global__ __launch_bounds__(R::LB) void k_top(const void* logits, size_t ld, in
     if (threadIdx.x == 0)
       lse[blockIdx.x] = fabsf(m) < INFINITY ? (float)((double)m + log(sum)) : m;
   }
-  first_tokens(row, t, n, s, g);
+  first_tokens(row, t, n, s, g, [&](float x) { return row.reach(x); });
   if ((int)threadIdx.x < n) {
     const size_t o = (size_t)blockIdx.x * n + threadIdx.x;
     const uint64_t top = s.sorted[threadIdx.x];
@@ -1335,7 +1369,8 @@ __global__ __launch_bounds__(R::LB) void k_distill(const void* logits, size_t ld
     }
   }
   const float c = (float)(t.inv_t * M_LOG2E);
-  const Online on = online<false>(row, c);
+  Online on;
+  row.template each<4>([&](int, int, const u32x4& u) { add_unit<false, R>(on, u, c); });
   // the entries' logits are read before a gradient in their place is written
   asm volatile("" ::"v"(zk));
   // (a NaN is passed over here and found again by the sum)
@@ -1412,6 +1447,24 @@ void by_row(int rows, int cols, F f) {
   f(Tag<HeldRow<TYPE, 1024, 0>>());
 }
 
+// The same of rows that keep their units' largest.
+template <int TYPE, class F>
+void by_tops(int rows, int cols, F f) {
+  constexpr int MOST = LOGITS_MAX_COLS / (1024 * Type<TYPE>::E);
+  using Short = ToppedRow<TYPE, 256, 8, 8>;
+  // rows that share a CU hide each other's reading; a row alone has all of it under way
+  using Two = ToppedRow<TYPE, 512, 16, 8>;
+  using LongTwo = ToppedRow<TYPE, 512, 38, 6>;
+  using One = ToppedRow<TYPE, 1024, 8, 8>;
+  using LongOne = ToppedRow<TYPE, 1024, 18, 18>;
+  if (cols * Type<TYPE>::SIZE <= SHORT_ROW) return f(Tag<Short>());
+  if (rows > 256 && holds<Two>(cols)) return f(Tag<Two>());
+  if (rows > 256 && holds<LongTwo>(cols)) return f(Tag<LongTwo>());
+  if (holds<One>(cols)) return f(Tag<One>());
+  if (holds<LongOne>(cols)) return f(Tag<LongOne>());
+  f(Tag<ToppedRow<TYPE, 1024, MOST, 6>>());
+}
+
 template <int TYPE, class F>
 void by_runs(int rows, int cols, F f) {
   if (cols * Type<TYPE>::SIZE <= SHORT_ROW)
@@ -1428,7 +1481,7 @@ void launch_logits_top(const void* x, int type, size_t ld, int rows, int cols, i
                        int* ids, float* lse, hipStream_t st) {
   if (rows <= 0) return;
   by_type(type, [&](auto t) {
-    by_row<t(), 18, true>(rows, cols, [&](auto r) {
+    by_tops<t()>(rows, cols, [&](auto r) {
       using R = typename decltype(r)::type;
       k_top<R><<<rows, R::LB, 0, st>>>(x, ld, cols, k, values, ids, lse);
     });
@@ -1442,7 +1495,7 @@ void launch_logits_sample(const void* x, int type, size_t ld, int rows, int cols
   const bool few = how.top_k > 0 && how.top_k <= LOGITS_TOP_MAX;
   by_type(type, [&](auto t) {
     if (few)
-      by_row<t(), 18, false>(rows, cols, [&](auto r) {
+      by_tops<t()>(rows, cols, [&](auto r) {
         using R = typename decltype(r)::type;
         k_sample_few<R><<<rows, R::LB, 0, st>>>(x, ld, cols, how, uniforms, tokens, logprobs);
       });
@@ -1478,10 +1531,15 @@ void launch_logits_distill(const void* x, int type, size_t ld, int rows, int col
                            void* dx, size_t ldd, hipStream_t st) {
   if (rows <= 0) return;
   by_type(type, [&](auto t) {
-    by_row<t(), 18, true>(rows, cols, [&](auto r) {
+    const auto run = [&](auto r) {
       using R = typename decltype(r)::type;
       k_distill<R><<<rows, R::LB, 0, st>>>(x, ld, cols, t_, loss, lse, grad, dx, ldd);
-    });
+    };
+    // without a gradient a row is read once, and need not be held
+    if (!dx && rows > 256 && cols * Type<t()>::SIZE > SHORT_ROW)
+      run(Tag<HeldRow<t(), 512, 0>>());
+    else
+      by_row<t(), 18, true>(rows, cols, run);
   });
 }
 
