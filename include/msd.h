@@ -144,6 +144,20 @@ typedef struct msd_tree {
 
 typedef struct msd_ctx msd_ctx;
 
+/* Which tokens of a row of logits stay (msd_logits_sample has the rules). */
+typedef struct msd_sampling {
+  double temperature, top_p, min_p;
+  int32_t top_k;
+} msd_sampling;
+
+/* A teacher's top logits (msd_logits_distill). */
+typedef struct msd_teacher {
+  const int32_t* ids_d;
+  const float* values_d;
+  int32_t k;
+  double temperature;
+} msd_teacher;
+
 /* Byte sizes of the caller-owned buffers for this shape and these limits
  * (any output pointer may be NULL).  Errors: MSD_ERR_INVALID_ARG for a shape
  * or limit outside the documented ranges. */
@@ -186,6 +200,17 @@ const char* msd_last_error(const msd_ctx* ctx);
 int msd_prefill(msd_ctx* ctx, int seq, int n, const int32_t* tokens_h,
                 const uint8_t* is_visual_h, const void* visual_d,
                 int32_t* first_token_h);
+
+/*
+ * msd_prefill whose first token is drawn, as msd_logits_sample does, from the target's
+ * distribution under `how` with the uniform number u (0 <= u < 1), so that decoding
+ * at a temperature samples from its first token on.  A prompt whose logits are all NaN
+ * or -inf gets msd_prefill's token.  Errors as of msd_prefill and, for the settings, of
+ * msd_logits_sample (on the context).
+ */
+int msd_prefill_sample(msd_ctx* ctx, int seq, int n, const int32_t* tokens_h,
+                       const uint8_t* is_visual_h, const void* visual_d, const msd_sampling* how,
+                       float u, int32_t* first_token_h);
 
 /*
  * Draft input of the visual prompt rows (the input-decoupling ablation,
@@ -408,6 +433,22 @@ int msd_set_state(msd_ctx* ctx, int seq, int L, const void* h_d, int32_t next_to
  */
 int msd_train_accumulate(msd_ctx* ctx, int seq, int n, const int32_t* tokens_h,
                          const uint8_t* is_visual_h, const void* visual_d, double* loss_h);
+/*
+ * Training from a teacher's record.  msd_train_record runs the target over a sequence (its
+ * arguments as for msd_train_accumulate, as is what it does to the slot) and writes the k
+ * largest logits of W_lm h_{i+1} for i = 0 .. n-2 (values_d and ids_d [n - 1][k], lse_d
+ * [n - 1] or NULL, as of msd_logits_top; enqueued, not waited for).
+ * msd_train_accumulate_top is msd_train_accumulate with such a record (or any other
+ * teacher's) in place of the target's distribution: the token part of loss_i is
+ * msd_logits_distill's loss of row i of the record and the draft's logits W_lm d_i, at the
+ * teacher's temperature.  It saves the LM head over the target's features.
+ */
+int msd_train_record(msd_ctx* ctx, int seq, int n, const int32_t* tokens_h,
+                     const uint8_t* is_visual_h, const void* visual_d, int k, float* values_d,
+                     int32_t* ids_d, float* lse_d);
+int msd_train_accumulate_top(msd_ctx* ctx, int seq, int n, const int32_t* tokens_h,
+                             const uint8_t* is_visual_h, const void* visual_d,
+                             const msd_teacher* teacher, double* loss_h);
 int msd_train_apply(msd_ctx* ctx, double lr);
 int msd_train_read(msd_ctx* ctx, int what, float* out_d, size_t n_floats);
 int msd_train_lr(int step, int total_steps, double lr_max, double* lr_out);
@@ -512,11 +553,8 @@ int msd_logits_top(const void* logits_d, int type, size_t ld, int rows, int cols
  * Those with a logit of -inf never do; any other row keeps its first token.  temperature 0
  * keeps the first token alone; else it is positive and finite.  Weights are computed in 64 bits and summed as
  * whole numbers of 2^-45, so that borders do not depend on an order of summation.
+ * (msd_sampling, above.)
  */
-typedef struct msd_sampling {
-  double temperature, top_p, min_p;
-  int32_t top_k;
-} msd_sampling;
 
 /* One token of every row, drawn from those that stay with probabilities in the ratio of
  * their weights: the first id whose running sum of weights (in the order of ids) exceeds
@@ -550,12 +588,6 @@ int msd_logits_filter(const void* logits_d, int type, size_t ld, int rows, int c
  * infinite (the gradient is not).  A NaN, or an infinite value other than -inf, makes
  * its row NaN; so does a student's row of -inf.
  */
-typedef struct msd_teacher {
-  const int32_t* ids_d;
-  const float* values_d;
-  int32_t k;
-  double temperature;
-} msd_teacher;
 int msd_logits_distill(const void* logits_d, int type, size_t ld, int rows, int cols,
                        const msd_teacher* teacher, float* loss_d, float* lse_d,
                        const float* grad_d, void* dlogits_d, size_t ldd, void* stream);

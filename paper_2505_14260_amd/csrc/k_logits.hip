@@ -1126,16 +1126,16 @@ MSD_DEV void put_token(int id, float x, uint64_t all, const Scale& sc, int* toke
     logprobs[blockIdx.x] = (float)((x == sc.m ? 0.0 : ((double)x - sc.m64) * sc.c * M_LN2) -
                                    log((double)all * (1 / ONE)));
 }
-MSD_DEV void put_no_token(int* tokens, float* logprobs) {
+MSD_DEV void put_no_token(int* tokens, float* logprobs, bool keep) {
   if (threadIdx.x) return;
-  tokens[blockIdx.x] = -1;
+  if (!keep) tokens[blockIdx.x] = -1;
   if (logprobs) logprobs[blockIdx.x] = -INFINITY;
 }
 
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_sample_few(const void* logits, size_t ld, int V,
                                                       LogitsChoice how, const float* uniforms,
-                                                      int* tokens, float* logprobs) {
+                                                      int* tokens, float* logprobs, bool keep) {
   __shared__ FewLds s;
   Group<R::W> g{s};
   const float u = uniforms[blockIdx.x];
@@ -1148,7 +1148,7 @@ __global__ __launch_bounds__(R::LB) void k_sample_few(const void* logits, size_t
     return m;
   });
   const Tops t = tops(key_of(mine), (min(how.top_k, V) + R::W - 1) / R::W, g);
-  if (t.max <= KEY_NINF) return put_no_token(tokens, logprobs);
+  if (t.max <= KEY_NINF) return put_no_token(tokens, logprobs, keep);
   const Scale sc(of_key(t.max), how.c);
   uint64_t all;
   const int n = choose_few(row, t, sc, how, &all, s, g, [&](float x) { return row.reach(x); });
@@ -1165,7 +1165,7 @@ __global__ __launch_bounds__(R::LB) void k_sample_few(const void* logits, size_t
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_sample_many(const void* logits, size_t ld, int V,
                                                        LogitsChoice how, const float* uniforms,
-                                                       int* tokens, float* logprobs) {
+                                                       int* tokens, float* logprobs, bool keep) {
   __shared__ ManyLds s;
   Group<R::W> g{s};
   const float u = uniforms[blockIdx.x];
@@ -1173,7 +1173,7 @@ __global__ __launch_bounds__(R::LB) void k_sample_many(const void* logits, size_
   for (int i = threadIdx.x; i < CELLS; i += R::LB) s.cells[i] = 0;
   float ref = 0.f;
   const float m = largest(row, how.c, how.top_p < 1, &ref, s, g);
-  if (!(m > -INFINITY)) return put_no_token(tokens, logprobs);
+  if (!(m > -INFINITY)) return put_no_token(tokens, logprobs, keep);
   const Scale sc(m, how.c);
   const Start st = start_many(row, ref, sc, how, s, g);
   Kept k = st.plan.above;
@@ -1490,19 +1490,19 @@ void launch_logits_top(const void* x, int type, size_t ld, int rows, int cols, i
 
 void launch_logits_sample(const void* x, int type, size_t ld, int rows, int cols,
                           const LogitsChoice& how, const float* uniforms, int* tokens,
-                          float* logprobs, hipStream_t st) {
+                          float* logprobs, hipStream_t st, bool keep) {
   if (rows <= 0) return;
   const bool few = how.top_k > 0 && how.top_k <= LOGITS_TOP_MAX;
   by_type(type, [&](auto t) {
     if (few)
       by_tops<t()>(rows, cols, [&](auto r) {
         using R = typename decltype(r)::type;
-        k_sample_few<R><<<rows, R::LB, 0, st>>>(x, ld, cols, how, uniforms, tokens, logprobs);
+        k_sample_few<R><<<rows, R::LB, 0, st>>>(x, ld, cols, how, uniforms, tokens, logprobs, keep);
       });
     else
       by_runs<t()>(rows, cols, [&](auto r) {
         using R = typename decltype(r)::type;
-        k_sample_many<R><<<rows, R::LB, 0, st>>>(x, ld, cols, how, uniforms, tokens, logprobs);
+        k_sample_many<R><<<rows, R::LB, 0, st>>>(x, ld, cols, how, uniforms, tokens, logprobs, keep);
       });
   });
 }

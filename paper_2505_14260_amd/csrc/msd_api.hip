@@ -1541,10 +1541,20 @@ int train_init(msd_ctx* c) {
   return MSD_OK;
 }
 
+// The target's logits of rows 1 .. R of a training sequence, in t->Lt.
+int train_target_logits(msd_ctx* c, int R) {
+  TrainState* t = c->tr;
+  const int d = c->m.d_model;
+  // its features are the split rows of the target pass
+  return train_gemm(c, c->h + 2 * (size_t)d, R, d, 2, c->lm_p, t->Vp, 1, 0, t->Lt, t->Vp, nullptr);
+}
+
 // One training sequence: forward, loss and gradient sums (see
 // msd_train_accumulate).  c->h holds the target features of its n rows,
-// c->rows.tok / .vis its tokens and visual row indices.
-int train_pass(msd_ctx* c, int n, const void* visual_d, double* loss3) {
+// c->rows.tok / .vis its tokens and visual row indices.  top: the token term's teacher, in
+// place of the target's distribution of those features.
+int train_pass(msd_ctx* c, int n, const void* visual_d, double* loss3,
+               const LogitsTeacher* top = nullptr) {
   TrainState* t = c->tr;
   const msd_model_desc& m = c->m;
   const int d = m.d_model, F = m.ffn_dim, H = m.n_heads, KV = m.n_kv_heads, hd = m.head_dim;
@@ -1589,9 +1599,13 @@ int train_pass(msd_ctx* c, int n, const void* visual_d, double* loss3) {
   tr_split(t->D, R, d, t->xs, st);
   LAUNCHED(c);
   TRY(train_gemm(c, t->xs, R, d, 3, c->lm_p, t->Vp, 1, 0, t->Ld, t->Vp, nullptr));
-  // the target's features are the split rows of the target pass
-  TRY(train_gemm(c, c->h + 2 * (size_t)d, R, d, 2, c->lm_p, t->Vp, 1, 0, t->Lt, t->Vp, nullptr));
-  tr_ce(t->Ld, t->Lt, R, V, t->Vp, TRAIN_CLS_WEIGHT, t->ce, st);
+  if (top) {
+    tr_fill(t->Lt, R, TRAIN_CLS_WEIGHT, st);
+    launch_logits_distill(t->Ld, MX_F32, t->Vp, R, V, *top, t->ce, nullptr, t->Lt, t->Ld, t->Vp, st);
+  } else {
+    TRY(train_target_logits(c, R));
+    tr_ce(t->Ld, t->Lt, R, V, t->Vp, TRAIN_CLS_WEIGHT, t->ce, st);
+  }
   tr_split(t->Ld, R, t->Vp, t->xs, st);
   LAUNCHED(c);
   TRY(train_gemm(c, t->xs, R, t->Vp, 3, t->lm_t, d, 1, 0, t->dD, d, t->dD));
@@ -1639,6 +1653,104 @@ int train_pass(msd_ctx* c, int n, const void* visual_d, double* loss3) {
   loss3[1] = reg;
   loss3[2] = ce;
   t->rows += R;
+  return MSD_OK;
+}
+
+// The checks of a training sequence, the training state and the target's features of the
+// sequence.
+int train_target(msd_ctx* c, int seq, int n, const int32_t* tokens_h, const uint8_t* is_visual_h,
+                 const void* visual_d) {
+  if (!c) return fail(nullptr, MSD_ERR_INVALID_ARG, "null context");
+  const msd_model_desc& m = c->m;
+  if (seq < 0 || seq >= c->lim.max_batch) return fail(c, MSD_ERR_INVALID_ARG, "bad sequence");
+  if (n < 2 || n > c->lim.max_prompt || n > c->lim.max_seq || !tokens_h || !is_visual_h)
+    return fail(c, MSD_ERR_INVALID_ARG, "bad training sequence");
+  int n_vis = 0;
+  for (int i = 0; i < n; ++i) {
+    if (!is_visual_h[i] && (tokens_h[i] < 0 || tokens_h[i] >= m.vocab))
+      return fail(c, MSD_ERR_INVALID_ARG, "token id out of range");
+    n_vis += is_visual_h[i] ? 1 : 0;
+  }
+  if (n_vis && !visual_d) return fail(c, MSD_ERR_INVALID_ARG, "visual rows missing");
+  TRY(train_init(c));
+  c->verified_T = 0;
+  // the slot's cache now holds the training sequence: no longer a decode state
+  c->ready[seq] = 0;
+  c->L[seq] = 0;
+  // the slots' bytes were activations of the last sequence
+  c->tr->feature.src[0] = c->tr->feature.src[1] = nullptr;
+  return prompt_target(c, seq, n, tokens_h, is_visual_h, visual_d, true, true);
+}
+
+bool teacher_settings(const msd_teacher& t, LogitsTeacher* out) {
+  *out = LogitsTeacher{t.ids_d, t.values_d, t.k, 1 / t.temperature};
+  return t.k >= 1 && t.k <= LOGITS_TOP_MAX && t.temperature >= 1e-6 && t.temperature <= 1e6;
+}
+
+// Which tokens stay; null where the settings are good, else what they want.
+const char* sampling_settings(const msd_sampling* s, LogitsChoice* out) {
+  if (!s) return "null sampling settings";
+  if (!(s->temperature >= 0) || !std::isfinite(s->temperature))
+    return "sampling: temperature must be finite and not negative";
+  if (s->top_k < 0 || !(s->top_p > 0 && s->top_p <= 1) || !(s->min_p >= 0 && s->min_p <= 1))
+    return "sampling: wants top_k >= 0, 0 < top_p <= 1 and 0 <= min_p <= 1";
+  const bool greedy = s->temperature == 0;
+  const double T = greedy ? 1 : s->temperature;
+  *out = LogitsChoice{std::min(M_LOG2E / T, 1e300), s->top_p,
+                      s->min_p > 0 ? T * std::log(s->min_p) : -INFINITY, greedy ? 1 : s->top_k};
+  return nullptr;
+}
+
+// msd_prefill; with `how` the first token is drawn with the uniform number u.
+int prefill(msd_ctx* c, int seq, int n, const int32_t* tokens_h, const uint8_t* is_visual_h,
+            const void* visual_d, const LogitsChoice* how, float u, int32_t* first_token_h) {
+  if (!c) return fail(nullptr, MSD_ERR_INVALID_ARG, "null context");
+  const msd_model_desc& m = c->m;
+  if (seq < 0 || seq >= c->lim.max_batch) return fail(c, MSD_ERR_INVALID_ARG, "bad sequence");
+  if (n <= 0 || n > c->lim.max_prompt || !tokens_h || !is_visual_h || !first_token_h)
+    return fail(c, MSD_ERR_INVALID_ARG, "bad prompt");
+  if (n + c->lim.max_tree > c->lim.max_seq)
+    return fail(c, MSD_ERR_CAPACITY, "prompt does not fit the KV cache");
+  if (is_visual_h[n - 1]) return fail(c, MSD_ERR_INVALID_ARG, "prompt must end in a text token");
+  c->verified_T = 0;  // a prompt invalidates a pending verify (it rewrites the features)
+  int n_vis = 0;
+  for (int i = 0; i < n; ++i) {
+    if (!is_visual_h[i] && (tokens_h[i] < 0 || tokens_h[i] >= m.vocab))
+      return fail(c, MSD_ERR_INVALID_ARG, "token id out of range");
+    n_vis += is_visual_h[i] ? 1 : 0;
+  }
+  if (n_vis && !visual_d) return fail(c, MSD_ERR_INVALID_ARG, "visual rows missing");
+  const bool all = c->visual_input == MSD_DRAFT_VISUAL_FEATURE;  // features wanted of every row
+  TRY(prompt_target(c, seq, n, tokens_h, is_visual_h, visual_d, all));
+  const int d = m.d_model;
+  const int n_text = n - n_vis;
+  // (the GEMM with an argmax leaves the partials' place to the logits)
+  TRY(lm_argmax(c, c->h + (size_t)((all ? n : n_text) - 1) * 2 * d, 1, c->tk_idx,
+                how ? c->part : nullptr));
+  if (how) {
+    TRY(upload_many(c, {{c->tk_val, &u, sizeof(float)}}));
+    launch_logits_sample(c->part, MX_F32, m.vocab, 1, m.vocab, *how, c->tk_val, c->tk_idx, nullptr,
+                         c->st, true);
+    LAUNCHED(c);
+  }
+  launch_set_int(c->d_root, seq, c->tk_idx, 0, c->st);
+  launch_set_int(c->nxt, n_text - 1, c->tk_idx, 0, c->st);
+  LAUNCHED(c);
+  // draft over the prompt: text rows f_down(Concat(h_i, e_{i+1})), visual rows
+  // e_i (or h_i for the Visual Feature input)
+  launch_fc_input(c->h, nullptr, all ? c->rows.hrow : nullptr, c->embed, c->nxt,
+                  (const uint16_t*)visual_d, n_text, d, c->fcin, c->st);
+  LAUNCHED(c);
+  TRY(draft_prompt(c, n, n_text, (const uint16_t*)visual_d));
+  int st_len[2] = {n, 0};
+  TRY(upload_many(c, {{c->d_len + seq, st_len, sizeof(int)}, {c->pend_n + seq, st_len + 1, sizeof(int)}}));
+  int* back = c->stage + STAGE_INTS - 64;
+  HIPC(c, hipMemcpyAsync(back, c->d_root + seq, sizeof(int), hipMemcpyDeviceToHost, c->st));
+  HIPC(c, hipStreamSynchronize(c->st));
+  *first_token_h = back[0];
+  c->L[seq] = n;
+  c->pend[seq] = 0;
+  c->ready[seq] = 1;
   return MSD_OK;
 }
 
@@ -1801,46 +1913,16 @@ int msd_seq_len(const msd_ctx* c, int seq) {
 
 int msd_prefill(msd_ctx* c, int seq, int n, const int32_t* tokens_h, const uint8_t* is_visual_h,
                 const void* visual_d, int32_t* first_token_h) {
-  if (!c) return fail(nullptr, MSD_ERR_INVALID_ARG, "null context");
-  const msd_model_desc& m = c->m;
-  if (seq < 0 || seq >= c->lim.max_batch) return fail(c, MSD_ERR_INVALID_ARG, "bad sequence");
-  if (n <= 0 || n > c->lim.max_prompt || !tokens_h || !is_visual_h || !first_token_h)
-    return fail(c, MSD_ERR_INVALID_ARG, "bad prompt");
-  if (n + c->lim.max_tree > c->lim.max_seq)
-    return fail(c, MSD_ERR_CAPACITY, "prompt does not fit the KV cache");
-  if (is_visual_h[n - 1]) return fail(c, MSD_ERR_INVALID_ARG, "prompt must end in a text token");
-  c->verified_T = 0;  // a prompt invalidates a pending verify (it rewrites the features)
-  int n_vis = 0;
-  for (int i = 0; i < n; ++i) {
-    if (!is_visual_h[i] && (tokens_h[i] < 0 || tokens_h[i] >= m.vocab))
-      return fail(c, MSD_ERR_INVALID_ARG, "token id out of range");
-    n_vis += is_visual_h[i] ? 1 : 0;
-  }
-  if (n_vis && !visual_d) return fail(c, MSD_ERR_INVALID_ARG, "visual rows missing");
-  const bool all = c->visual_input == MSD_DRAFT_VISUAL_FEATURE;  // features wanted of every row
-  TRY(prompt_target(c, seq, n, tokens_h, is_visual_h, visual_d, all));
-  const int d = m.d_model;
-  const int n_text = n - n_vis;
-  TRY(lm_argmax(c, c->h + (size_t)((all ? n : n_text) - 1) * 2 * d, 1, c->tk_idx, nullptr));
-  launch_set_int(c->d_root, seq, c->tk_idx, 0, c->st);
-  launch_set_int(c->nxt, n_text - 1, c->tk_idx, 0, c->st);
-  LAUNCHED(c);
-  // draft over the prompt: text rows f_down(Concat(h_i, e_{i+1})), visual rows
-  // e_i (or h_i for the Visual Feature input)
-  launch_fc_input(c->h, nullptr, all ? c->rows.hrow : nullptr, c->embed, c->nxt,
-                  (const uint16_t*)visual_d, n_text, d, c->fcin, c->st);
-  LAUNCHED(c);
-  TRY(draft_prompt(c, n, n_text, (const uint16_t*)visual_d));
-  int st_len[2] = {n, 0};
-  TRY(upload_many(c, {{c->d_len + seq, st_len, sizeof(int)}, {c->pend_n + seq, st_len + 1, sizeof(int)}}));
-  int* back = c->stage + STAGE_INTS - 64;
-  HIPC(c, hipMemcpyAsync(back, c->d_root + seq, sizeof(int), hipMemcpyDeviceToHost, c->st));
-  HIPC(c, hipStreamSynchronize(c->st));
-  *first_token_h = back[0];
-  c->L[seq] = n;
-  c->pend[seq] = 0;
-  c->ready[seq] = 1;
-  return MSD_OK;
+  return prefill(c, seq, n, tokens_h, is_visual_h, visual_d, nullptr, 0.f, first_token_h);
+}
+
+int msd_prefill_sample(msd_ctx* c, int seq, int n, const int32_t* tokens_h,
+                       const uint8_t* is_visual_h, const void* visual_d, const msd_sampling* how,
+                       float u, int32_t* first_token_h) {
+  LogitsChoice choice;
+  if (c)
+    if (const char* wrong = sampling_settings(how, &choice)) return fail(c, MSD_ERR_INVALID_ARG, wrong);
+  return prefill(c, seq, n, tokens_h, is_visual_h, visual_d, &choice, u, first_token_h);
 }
 
 int msd_set_draft_input(msd_ctx* c, int visual_input) {
@@ -2187,28 +2269,37 @@ int msd_stream_read(const void* buf_d, size_t bytes, int workgroups, void* sink_
 
 int msd_train_accumulate(msd_ctx* c, int seq, int n, const int32_t* tokens_h,
                          const uint8_t* is_visual_h, const void* visual_d, double* loss_h) {
-  if (!c) return fail(nullptr, MSD_ERR_INVALID_ARG, "null context");
-  const msd_model_desc& m = c->m;
-  if (seq < 0 || seq >= c->lim.max_batch) return fail(c, MSD_ERR_INVALID_ARG, "bad sequence");
-  if (n < 2 || n > c->lim.max_prompt || n > c->lim.max_seq || !tokens_h || !is_visual_h ||
-      !loss_h)
-    return fail(c, MSD_ERR_INVALID_ARG, "bad training sequence");
-  int n_vis = 0;
-  for (int i = 0; i < n; ++i) {
-    if (!is_visual_h[i] && (tokens_h[i] < 0 || tokens_h[i] >= m.vocab))
-      return fail(c, MSD_ERR_INVALID_ARG, "token id out of range");
-    n_vis += is_visual_h[i] ? 1 : 0;
-  }
-  if (n_vis && !visual_d) return fail(c, MSD_ERR_INVALID_ARG, "visual rows missing");
-  TRY(train_init(c));
-  c->verified_T = 0;
-  // the slot's cache now holds the training sequence: no longer a decode state
-  c->ready[seq] = 0;
-  c->L[seq] = 0;
-  // the slots' bytes were activations of the last sequence
-  c->tr->feature.src[0] = c->tr->feature.src[1] = nullptr;
-  TRY(prompt_target(c, seq, n, tokens_h, is_visual_h, visual_d, true, true));
+  if (c && !loss_h) return fail(c, MSD_ERR_INVALID_ARG, "null loss output");
+  TRY(train_target(c, seq, n, tokens_h, is_visual_h, visual_d));
   return train_pass(c, n, visual_d, loss_h);
+}
+
+int msd_train_accumulate_top(msd_ctx* c, int seq, int n, const int32_t* tokens_h,
+                             const uint8_t* is_visual_h, const void* visual_d,
+                             const msd_teacher* teacher, double* loss_h) {
+  if (!c) return fail(nullptr, MSD_ERR_INVALID_ARG, "null context");
+  LogitsTeacher top;
+  if (!loss_h || !teacher || !teacher->ids_d || !teacher->values_d ||
+      ((uintptr_t)teacher->ids_d & 3) || ((uintptr_t)teacher->values_d & 3) ||
+      !teacher_settings(*teacher, &top))
+    return fail(c, MSD_ERR_INVALID_ARG, "bad teacher, or null loss output");
+  TRY(train_target(c, seq, n, tokens_h, is_visual_h, visual_d));
+  return train_pass(c, n, visual_d, loss_h, &top);
+}
+
+int msd_train_record(msd_ctx* c, int seq, int n, const int32_t* tokens_h,
+                     const uint8_t* is_visual_h, const void* visual_d, int k, float* values_d,
+                     int32_t* ids_d, float* lse_d) {
+  if (!c) return fail(nullptr, MSD_ERR_INVALID_ARG, "null context");
+  if (k < 1 || k > std::min(LOGITS_TOP_MAX, c->m.vocab) || !values_d || !ids_d ||
+      (((uintptr_t)values_d | (uintptr_t)ids_d | (uintptr_t)lse_d) & 3))
+    return fail(c, MSD_ERR_INVALID_ARG, "bad record: k, or null or misaligned outputs");
+  TRY(train_target(c, seq, n, tokens_h, is_visual_h, visual_d));
+  TRY(train_target_logits(c, n - 1));
+  launch_logits_top(c->tr->Lt, MX_F32, c->tr->Vp, n - 1, c->m.vocab, k, values_d, ids_d, lse_d,
+                    c->st);
+  LAUNCHED(c);
+  return MSD_OK;
 }
 
 int msd_train_apply(msd_ctx* c, double lr) {
@@ -2492,17 +2583,8 @@ int logits_array(const void* p, size_t n, bool needed, Span* out) {
 }
 
 int logits_choice(const msd_sampling* s, LogitsChoice* out) {
-  if (!s) return mx_fail(MSD_ERR_INVALID_ARG, "logits: null settings");
-  if (!(s->temperature >= 0) || !std::isfinite(s->temperature))
-    return mx_fail(MSD_ERR_INVALID_ARG, "logits: temperature must be finite and not negative");
-  if (s->top_k < 0 || !(s->top_p > 0 && s->top_p <= 1) || !(s->min_p >= 0 && s->min_p <= 1))
-    return mx_fail(MSD_ERR_INVALID_ARG,
-                   "logits: wants top_k >= 0, 0 < top_p <= 1 and 0 <= min_p <= 1");
-  const bool greedy = s->temperature == 0;
-  const double T = greedy ? 1 : s->temperature;
-  *out = LogitsChoice{std::min(M_LOG2E / T, 1e300), s->top_p, s->min_p > 0 ? T * std::log(s->min_p) : -INFINITY,
-                      greedy ? 1 : s->top_k};
-  return MSD_OK;
+  const char* wrong = sampling_settings(s, out);
+  return wrong ? mx_fail(MSD_ERR_INVALID_ARG, wrong) : MSD_OK;
 }
 
 }  // namespace
@@ -2560,10 +2642,10 @@ int msd_logits_distill(const void* logits_d, int type, size_t ld, int rows, int 
                        const float* grad_d, void* dlogits_d, size_t ldd, void* stream) {
   Span x, ids, vals, l, e, g, dx{nullptr, 0};
   TRY(logits_float(logits_d, type, ld, rows, cols, &x));
-  if (!teacher || teacher->k < 1 || teacher->k > LOGITS_TOP_MAX)
-    return mx_fail(MSD_ERR_INVALID_ARG, "distill: wants a teacher of 1 .. 256 entries a row");
-  if (!(teacher->temperature >= 1e-6 && teacher->temperature <= 1e6))
-    return mx_fail(MSD_ERR_INVALID_ARG, "distill: temperature must be 1e-6 .. 1e6");
+  LogitsTeacher t;
+  if (!teacher || !teacher_settings(*teacher, &t))
+    return mx_fail(MSD_ERR_INVALID_ARG,
+                   "distill: wants a teacher of 1 .. 256 entries a row, temperature 1e-6 .. 1e6");
   if (rows && ((!grad_d != !dlogits_d) || (!loss_d && !lse_d && !dlogits_d)))
     return mx_fail(MSD_ERR_INVALID_ARG,
                    "distill: wants an output, and the rows' weights with the gradient");
@@ -2576,7 +2658,6 @@ int msd_logits_distill(const void* logits_d, int type, size_t ld, int rows, int 
   TRY(mx_disjoint({l, e}, {x, ids, vals, g}));
   const bool in_place = dlogits_d == logits_d && ldd == ld;
   TRY(mx_disjoint({dx, l, e}, {in_place ? Span{nullptr, 0} : x, ids, vals, g}));
-  const LogitsTeacher t{teacher->ids_d, teacher->values_d, teacher->k, 1 / teacher->temperature};
   launch_logits_distill(logits_d, type, ld, rows, cols, t, loss_d, lse_d, grad_d, dlogits_d, ldd,
                         (hipStream_t)stream);
   return mx_launched();

@@ -440,7 +440,7 @@ void launch_mx_product(const MxMat& x, const MxMat& w, void* out, int type, size
 constexpr int LOGITS_TOP_MAX = 256;      // entries of a row's top logits
 constexpr int LOGITS_MAX_COLS = 1 << 18;
 struct LogitsChoice {
-  double c;      // log2(e) / temperature
+  double c;      // log2(e) / temperature (finite)
   double top_p;  // 1: all
   double min_d;  // temperature * log(min_p); -inf: all
   int top_k;     // 0: all
@@ -453,9 +453,10 @@ struct LogitsTeacher {
 };
 void launch_logits_top(const void* x, int type, size_t ld, int rows, int cols, int k, float* values,
                        int* ids, float* lse, hipStream_t st);
+// keep: a row without tokens leaves its place as it was
 void launch_logits_sample(const void* x, int type, size_t ld, int rows, int cols,
                           const LogitsChoice& how, const float* uniforms, int* tokens,
-                          float* logprobs, hipStream_t st);
+                          float* logprobs, hipStream_t st, bool keep = false);
 void launch_logits_filter(const void* x, int type, size_t ld, int rows, int cols,
                           const LogitsChoice& how, void* out, size_t ldo, int* kept,
                           hipStream_t st);

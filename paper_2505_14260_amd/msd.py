@@ -120,6 +120,11 @@ def lib():
         L.msd_stream_read.argtypes = [c_vp, c_sz, ctypes.c_int, c_vp, c_vp]
         L.msd_train_accumulate.argtypes = [c_vp, ctypes.c_int, ctypes.c_int, P(c_i32),
                                            P(ctypes.c_uint8), c_vp, P(ctypes.c_double)]
+        L.msd_prefill_sample.argtypes = L.msd_prefill.argtypes[:-1] + [P(Sampling), c_f32, P(c_i32)]
+        L.msd_train_record.argtypes = L.msd_train_accumulate.argtypes[:-1] + [ctypes.c_int, c_vp, c_vp,
+                                                                              c_vp]
+        L.msd_train_accumulate_top.argtypes = L.msd_train_accumulate.argtypes[:-1] + [
+            P(Teacher), P(ctypes.c_double)]
         L.msd_train_apply.argtypes = [c_vp, ctypes.c_double]
         L.msd_train_read.argtypes = [c_vp, ctypes.c_int, c_vp, c_sz]
         L.msd_train_lr.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.c_double,
@@ -201,6 +206,16 @@ def msd_prefill(ctx, seq, tokens, is_visual, visual_ptr):
     return first.value
 
 
+def msd_prefill_sample(ctx, seq, tokens, is_visual, visual_ptr, how: Sampling, u):
+    tok, ptok = _i32(tokens)
+    vis = np.ascontiguousarray(is_visual, dtype=np.uint8)
+    first = c_i32()
+    _check(ctx, lib().msd_prefill_sample(ctx, seq, len(tok), ptok,
+                                         vis.ctypes.data_as(ctypes.POINTER(ctypes.c_uint8)),
+                                         visual_ptr, how, u, ctypes.byref(first)))
+    return first.value
+
+
 def msd_draft_tree(ctx, seqs, spec: TreeSpec, trees_ptr):
     s, ps = _i32(seqs)
     _check(ctx, lib().msd_draft_tree(ctx, len(s), ps, ctypes.byref(spec), trees_ptr))
@@ -275,6 +290,26 @@ def msd_train_accumulate(ctx, seq, tokens, is_visual, visual_ptr):
     _check(ctx, lib().msd_train_accumulate(ctx, seq, len(tok), ptok,
                                            vis.ctypes.data_as(ctypes.POINTER(ctypes.c_uint8)),
                                            visual_ptr, loss))
+    return tuple(loss)
+
+
+def msd_train_record(ctx, seq, tokens, is_visual, visual_ptr, k, values_ptr, ids_ptr, lse_ptr):
+    tok, ptok = _i32(tokens)
+    vis = np.ascontiguousarray(is_visual, dtype=np.uint8)
+    _check(ctx, lib().msd_train_record(ctx, seq, len(tok), ptok,
+                                       vis.ctypes.data_as(ctypes.POINTER(ctypes.c_uint8)),
+                                       visual_ptr, k, values_ptr, ids_ptr, lse_ptr))
+
+
+def msd_train_accumulate_top(ctx, seq, tokens, is_visual, visual_ptr, teacher: Teacher):
+    """msd_train_accumulate with a teacher's record in place of the target's
+    distribution."""
+    tok, ptok = _i32(tokens)
+    vis = np.ascontiguousarray(is_visual, dtype=np.uint8)
+    loss = (ctypes.c_double * 3)()
+    _check(ctx, lib().msd_train_accumulate_top(
+        ctx, seq, len(tok), ptok, vis.ctypes.data_as(ctypes.POINTER(ctypes.c_uint8)), visual_ptr,
+        teacher, loss))
     return tuple(loss)
 
 
@@ -396,6 +431,17 @@ def make_dynamic_spec(topk, depth, n_nodes):
     return TreeSpec(TREE_DYNAMIC, n_nodes, depth, topk, None, None)
 
 
+def draw_uniform(seed, seq, length, j):
+    """Draw j of the cycle of sequence slot `seq` that starts at a committed length
+    (msd_accept_sample): a multiple of 2^-24 in [0, 1)."""
+    mask = (1 << 64) - 1
+    n = seq << 40 | length << 8 | j
+    z = (seed + (n + 1) * 0x9E3779B97F4A7C15) & mask
+    z = (z ^ z >> 30) * 0xBF58476D1CE4E5B9 & mask
+    z = (z ^ z >> 27) * 0x94D049BB133111EB & mask
+    return ((z ^ z >> 31) >> 40) / (1 << 24)
+
+
 class Engine:
     """Owns device copies of the weights and the caller-side buffers."""
 
@@ -455,14 +501,51 @@ class Engine:
                                                  dtype=self.torch.uint8, device=self.dev)
         msd_set_draft_mx(self.ctx, self.draft_mx.data_ptr())
 
-    def train_accumulate(self, seq, tokens, is_visual, visual_bits):
-        """Gradient sums of one training sequence; returns its loss sums."""
-        vis_t = None
-        ptr = None
-        if visual_bits is not None and len(visual_bits):
-            vis_t = self.torch.from_numpy(np.ascontiguousarray(visual_bits).view(np.int16)).to(self.dev)
-            ptr = vis_t.data_ptr()
-        return msd_train_accumulate(self.ctx, seq, tokens, is_visual, ptr)
+    def _visual(self, visual_bits):
+        """Device copy of visual rows and its pointer (None for none)."""
+        if visual_bits is None or not len(visual_bits):
+            return None, None
+        t = self.torch.from_numpy(np.ascontiguousarray(visual_bits).view(np.int16)).to(self.dev)
+        return t, t.data_ptr()
+
+    def train_accumulate(self, seq, tokens, is_visual, visual_bits, teacher=None):
+        """Gradient sums of one training sequence; returns its loss sums.
+        teacher: (ids, values, temperature), a record of the sequence's n - 1 rows as
+        train_record() returns it, in place of the target's distribution."""
+        vis_t, ptr = self._visual(visual_bits)
+        if teacher is None:
+            return msd_train_accumulate(self.ctx, seq, tokens, is_visual, ptr)
+        torch = self.torch
+        ids, values, temperature = teacher
+        for t, dtype, what in ((ids, torch.int32, "ids"), (values, torch.float32, "values")):
+            if t.dtype != dtype or t.dim() != 2 or t.shape[0] != len(tokens) - 1 \
+                    or t.shape != ids.shape or not t.is_contiguous() or not t.is_cuda:
+                raise ValueError(f"teacher's {what}: wants contiguous {dtype} of {len(tokens) - 1} "
+                                 f"rows on the GPU, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        self.torch_stream.wait_stream(torch.cuda.current_stream(self.dev))
+        return msd_train_accumulate_top(
+            self.ctx, seq, tokens, is_visual, ptr,
+            Teacher(ids.data_ptr(), values.data_ptr(), ids.shape[1], temperature))
+
+    def train_record(self, seq, tokens, is_visual, visual_bits, k):
+        """The target's record of a training sequence for train_accumulate(): (ids, values)
+        [n - 1, k] of its largest logits, on the engine's stream."""
+        torch = self.torch
+        vis_t, ptr = self._visual(visual_bits)
+        shape = (max(len(tokens) - 1, 0), k)
+        with torch.cuda.stream(self.torch_stream):
+            ids = torch.empty(shape, dtype=torch.int32, device=self.dev)
+            values = torch.empty(shape, dtype=torch.float32, device=self.dev)
+        msd_train_record(self.ctx, seq, tokens, is_visual, ptr, k, values.data_ptr(),
+                         ids.data_ptr(), None)
+        current = torch.cuda.current_stream(self.dev)
+        if current != self.torch_stream:
+            current.wait_stream(self.torch_stream)
+            ids.record_stream(current)
+            values.record_stream(current)
+        if vis_t is not None:
+            vis_t.record_stream(self.torch_stream)
+        return ids, values
 
     def train_apply(self, lr):
         msd_train_apply(self.ctx, lr)
@@ -514,14 +597,13 @@ class Engine:
         dv = self.bufs_t[3].view(self.torch.int16).view(1, B, KV, hd, S)
         return tk, tv, dk, dv
 
-    def prefill(self, seq, tokens, is_visual, visual_bits):
-        vis_t = None
-        ptr = None
-        if visual_bits is not None and len(visual_bits):
-            vis_t = self.torch.from_numpy(np.ascontiguousarray(visual_bits).view(np.int16)).to(self.dev)
-            ptr = vis_t.data_ptr()
-        first = msd_prefill(self.ctx, seq, tokens, is_visual, ptr)
-        return first
+    def prefill(self, seq, tokens, is_visual, visual_bits, sampling=None, u=0.0):
+        """The first token of a prompt: the greedy one, or with a Sampling the one drawn
+        with the uniform number u."""
+        vis_t, ptr = self._visual(visual_bits)
+        if sampling is not None:
+            return msd_prefill_sample(self.ctx, seq, tokens, is_visual, ptr, sampling, u)
+        return msd_prefill(self.ctx, seq, tokens, is_visual, ptr)
 
     def new_trees(self, n_seq):
         return self.torch.zeros(n_seq * ctypes.sizeof(Tree), dtype=self.torch.uint8, device=self.dev)
@@ -555,9 +637,16 @@ class Engine:
         return em, slots
 
     def accept_sample(self, seqs, trees_t, n_nodes, logits, temperature, seed,
-                      want_slots=False):
-        """Acceptance by speculative sampling; logits: verify's float32 logits."""
+                      want_slots=False, top_k=0, top_p=1.0, min_p=0.0):
+        """Acceptance by speculative sampling; logits: verify's float32 logits.  With
+        top_k, top_p or min_p the emitted tokens follow the target's distribution
+        filtered by them (logits.filter)."""
         slots = None
+        if top_k or top_p != 1.0 or min_p:
+            from . import logits as ops
+            with self.torch.cuda.stream(self.torch_stream):
+                logits = ops.filter(logits, self.torch.empty_like(logits), temperature=temperature,
+                                    top_k=top_k, top_p=top_p, min_p=min_p)
         if want_slots:
             slots = self.torch.empty(len(seqs) * MAX_TREE, dtype=self.torch.int32, device=self.dev)
         em = msd_accept_sample(self.ctx, seqs, trees_t.data_ptr(), n_nodes, logits.data_ptr(),
@@ -565,12 +654,21 @@ class Engine:
                                slots.data_ptr() if slots is not None else None)
         return em, slots
 
-    def generate(self, seq, prompt, spec, n_new, record=False, temperature=0.0, seed=0):
+    def generate(self, seq, prompt, spec, n_new, record=False, temperature=0.0, seed=0,
+                 top_k=0, top_p=1.0, min_p=0.0, sample_first=False):
         """Speculative decoding of one sequence: n_new tokens, greedy at
-        temperature 0, else speculative sampling (the first token, from the
-        prompt, is the greedy one either way)."""
+        temperature 0, else speculative sampling, from the distribution that
+        top_k, top_p and min_p leave.  The first token, from the prompt, is the
+        greedy one either way unless sample_first draws it too (with draw 255 of
+        the cycle that starts at the prompt's length)."""
         tokens, is_visual, visual = prompt
-        out = [self.prefill(seq, tokens, is_visual, visual)]
+        how = dict(top_k=top_k, top_p=top_p, min_p=min_p)
+        if sample_first and temperature > 0:
+            out = [self.prefill(seq, tokens, is_visual, visual,
+                                Sampling(temperature, top_p, min_p, top_k),
+                                draw_uniform(seed, seq, len(tokens), 255))]
+        else:
+            out = [self.prefill(seq, tokens, is_visual, visual)]
         T = spec.n_nodes + 1
         trees = self.new_trees(1)
         cycles = []
@@ -578,7 +676,7 @@ class Engine:
             self.draft_tree([seq], spec, trees)
             amax, logits = self.verify([seq], trees, T, want_logits=temperature > 0)
             if temperature > 0:
-                em, _ = self.accept_sample([seq], trees, T, logits, temperature, seed)
+                em, _ = self.accept_sample([seq], trees, T, logits, temperature, seed, **how)
             else:
                 em, _ = self.accept([seq], trees, T, amax)
             out.extend(int(t) for t in em[0])
