@@ -650,14 +650,13 @@ MSD_DEV float unit_max(const u32x4& u) {
 }
 
 // The first n (at most LOGITS_TOP_MAX and V) tokens of the row in order, in s.sorted:
-// those that reach a bound that n at least do, ranked.  reach(x): the thread's units with
-// one that reaches x, a bit each; they are few, and read again.
-template <class R, class F>
-MSD_DEV void first_tokens(const R& row, const Tops& t, int n, FewLds& s, Group<R::W>& g, F reach) {
+// those that reach a bound that n at least do, ranked.
+template <class R>
+MSD_DEV void first_tokens(const R& row, const Tops& t, int n, FewLds& s, Group<R::W>& g) {
   const bool all = t.floor <= KEY_NINF;
   const float at_least = all ? -INFINITY : of_key(t.floor);
   const Row<R::T, R::LB>& mem = row;
-  uint64_t units = reach(at_least);
+  uint64_t units = row.reach(at_least);
   for (; units; units &= units - 1) {
     const int j = __ffsll((unsigned long long)units) - 1;
     append(mem, mem.id(j), mem.load_tail(j), s.list, FEW, s,
@@ -682,11 +681,11 @@ MSD_DEV void first_tokens(const R& row, const Tops& t, int n, FewLds& s, Group<R
 
 // The tokens that stay of a few at most (0 < top_k <= LOGITS_TOP_MAX): their number, in
 // order in s.sorted, with their weights in s.weights and *all their sum.
-template <class R, class F>
+template <class R>
 MSD_DEV int choose_few(const R& row, const Tops& t, const Scale& sc, const LogitsChoice& how,
-                       uint64_t* all, FewLds& s, Group<R::W>& g, F reach) {
+                       uint64_t* all, FewLds& s, Group<R::W>& g) {
   const int n = min(how.top_k, row.V);
-  first_tokens(row, t, n, s, g, reach);
+  first_tokens(row, t, n, s, g);
   uint32_t key = 0;
   uint64_t w = 0;
   if ((int)threadIdx.x < n) {
@@ -1032,27 +1031,33 @@ MSD_DEV uint32_t put_filtered(const R& row, char* o, Kept k) {
   return n;
 }
 
+// The row's first reading for a few first tokens.
+template <class R>
+MSD_DEV Tops read_tops(R& row, int n, Group<R::W>& g) {
+  float mine = -INFINITY;
+  row.read([&](const u32x4& u) {
+    const float m = unit_max<R>(u);
+    mine = fmaxf(mine, m);
+    return m;
+  });
+  return tops(key_of(mine), (min(n, row.V) + R::W - 1) / R::W, g);
+}
+
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_filter_few(const void* logits, size_t ld, int V,
                                                       LogitsChoice how, void* out, size_t ldo,
                                                       int* kept) {
   __shared__ FewLds s;
   Group<R::W> g{s};
-  const R row(logits, ld, V);
+  R row(logits, ld, V);
   char* const o = static_cast<char*>(out) + (size_t)blockIdx.x * ldo * Type<R::T>::SIZE;
   if (threadIdx.x == 0) s.count = 0;
-  const Tops t = tops(thread_max(row), (min(how.top_k, V) + R::W - 1) / R::W, g);
+  const Tops t = read_tops(row, how.top_k, g);
   Kept k{0xFF800000u, -1};  // nothing: +inf of no id
   int n = 0;
   if (t.max > KEY_NINF) {
     uint64_t all;
-    n = choose_few(row, t, Scale(of_key(t.max), how.c), how, &all, s, g, [&](float x) {
-      uint64_t units = 0;
-      row.template each<4>([&](int j, int, const u32x4& u) {
-        units |= (uint64_t)(unit_max<R>(u) >= x) << j;
-      });
-      return units;
-    });
+    n = choose_few(row, t, Scale(of_key(t.max), how.c), how, &all, s, g);
     const uint64_t last = s.sorted[n - 1];
     k = {(uint32_t)(last >> 32), (int)~(uint32_t)last};
   }
@@ -1141,17 +1146,11 @@ __global__ __launch_bounds__(R::LB) void k_sample_few(const void* logits, size_t
   const float u = uniforms[blockIdx.x];
   R row(logits, ld, V);
   if (threadIdx.x == 0) s.count = 0;
-  float mine = -INFINITY;
-  row.read([&](const u32x4& un) {
-    const float m = unit_max<R>(un);
-    mine = fmaxf(mine, m);
-    return m;
-  });
-  const Tops t = tops(key_of(mine), (min(how.top_k, V) + R::W - 1) / R::W, g);
+  const Tops t = read_tops(row, how.top_k, g);
   if (t.max <= KEY_NINF) return put_no_token(tokens, logprobs, keep);
   const Scale sc(of_key(t.max), how.c);
   uint64_t all;
-  const int n = choose_few(row, t, sc, how, &all, s, g, [&](float x) { return row.reach(x); });
+  const int n = choose_few(row, t, sc, how, &all, s, g);
   if ((int)threadIdx.x >= n) return;
   // the running sum in the order of the ids, of which ~ makes the lower the greater
   const uint32_t me = (uint32_t)s.sorted[threadIdx.x];
@@ -1285,7 +1284,7 @@ __global__ __launch_bounds__(R::LB) void k_top(const void* logits, size_t ld, in
     if (threadIdx.x == 0)
       lse[blockIdx.x] = fabsf(m) < INFINITY ? (float)((double)m + log(sum)) : m;
   }
-  first_tokens(row, t, n, s, g, [&](float x) { return row.reach(x); });
+  first_tokens(row, t, n, s, g);
   if ((int)threadIdx.x < n) {
     const size_t o = (size_t)blockIdx.x * n + threadIdx.x;
     const uint64_t top = s.sorted[threadIdx.x];
@@ -1434,16 +1433,19 @@ bool holds(int cols) {
   return cols / R::TILE <= R::UNITS;
 }
 
-// Calls f with a row type for each way to hold a row of `cols`: 256 threads for a short
-// one; up to LONG tiles of 1024 threads in registers; or read from memory in every pass.
-template <int TYPE, int LONG, bool SHARE, class F>
-void by_row(int rows, int cols, F f) {
-  if (cols * Type<TYPE>::SIZE <= SHORT_ROW) return f(Tag<HeldRow<TYPE, 256, 8>>());
-  if constexpr (SHARE)
-    if (rows > 256 && holds<HeldRow<TYPE, 512, 16>>(cols)) return f(Tag<HeldRow<TYPE, 512, 16>>());
-  if (holds<HeldRow<TYPE, 1024, 8>>(cols)) return f(Tag<HeldRow<TYPE, 1024, 8>>());
-  if constexpr (LONG > 0)
-    if (holds<HeldRow<TYPE, 1024, LONG>>(cols)) return f(Tag<HeldRow<TYPE, 1024, LONG>>());
+// Calls f with the type for a row of `cols` that is held: by 256 threads if it is short; by
+// 512, two rows to a CU, where there are more rows than CUs; by 1024; or read from memory
+// in every pass.
+template <int TYPE, class F>
+void by_held(int rows, int cols, F f) {
+  using Short = HeldRow<TYPE, 256, 8>;
+  using Two = HeldRow<TYPE, 512, 16>;
+  using One = HeldRow<TYPE, 1024, 8>;
+  using LongOne = HeldRow<TYPE, 1024, 18>;
+  if (cols * Type<TYPE>::SIZE <= SHORT_ROW) return f(Tag<Short>());
+  if (rows > 256 && holds<Two>(cols)) return f(Tag<Two>());
+  if (holds<One>(cols)) return f(Tag<One>());
+  if (holds<LongOne>(cols)) return f(Tag<LongOne>());
   f(Tag<HeldRow<TYPE, 1024, 0>>());
 }
 
@@ -1514,7 +1516,7 @@ void launch_logits_filter(const void* x, int type, size_t ld, int rows, int cols
   const bool few = how.top_k > 0 && how.top_k <= LOGITS_TOP_MAX;
   by_type(type, [&](auto t) {
     if (few)
-      by_row<t(), 18, false>(rows, cols, [&](auto r) {
+      by_tops<t()>(rows, cols, [&](auto r) {
         using R = typename decltype(r)::type;
         k_filter_few<R><<<rows, R::LB, 0, st>>>(x, ld, cols, how, out, ldo, kept);
       });
@@ -1539,7 +1541,7 @@ void launch_logits_distill(const void* x, int type, size_t ld, int rows, int col
     if (!dx && rows > 256 && cols * Type<t()>::SIZE > SHORT_ROW)
       run(Tag<HeldRow<t(), 512, 0>>());
     else
-      by_row<t(), 18, true>(rows, cols, run);
+      by_held<t()>(rows, cols, run);
   });
 }
 
