@@ -924,9 +924,10 @@ MSD_DEV Start start_many(const R& row, float ref, const Scale& sc, const LogitsC
 }
 
 // The pass that computes the weights of a row: the sums of all (with !EXACT) and of those
-// that surely stay, by cells too.  Units that hold tokens that only may stay are marked
-// and read again for the list, which they are few of.  f is called for each unit.
-template <bool EXACT, class R, class F>
+// that surely stay (with ALL: every token), by cells too.  Units that hold tokens that only
+// may stay are marked and read again for the list, which they are few of.  f is called for
+// each unit.
+template <bool EXACT, bool ALL, class R, class F>
 MSD_DEV void weigh(const R& row, const Scale& sc, const Start& st, uint64_t* all, uint64_t* above,
                    ManyLds& s, Group<R::W>& g, F f) {
   const Keeps stays(st.plan.above), within(st.limit);
@@ -953,12 +954,12 @@ MSD_DEV void weigh(const R& row, const Scale& sc, const Start& st, uint64_t* all
     }
 #pragma unroll
     for (int e = 0; e < R::E; ++e) {
-      in[e] = EXACT ? stays(x[e], i + e) : x[e] >= stays.x;
+      in[e] = ALL || (EXACT ? stays(x[e], i + e) : x[e] >= stays.x);
       any |= in[e];
       if (!EXACT) may |= x[e] >= low && !in[e];
     }
     if (!EXACT) marked |= (uint64_t)may << (j >> pairs);
-    if (!EXACT || __any(any)) {
+    if (ALL || !EXACT || __any(any)) {
       float z[R::E];
 #pragma unroll
       for (int e = 0; e < R::E; ++e) z[e] = x[e];
@@ -1061,7 +1062,19 @@ __global__ __launch_bounds__(R::LB) void k_filter_few(const void* logits, size_t
     const uint64_t last = s.sorted[n - 1];
     k = {(uint32_t)(last >> 32), (int)~(uint32_t)last};
   }
-  put_filtered(row, o, k);
+  // the few units with one of them are read again, and stored in their place
+  const uint64_t units = row.reach(of_key(k.key));
+  const Keeps stays(k);
+  for (int j = 0; j < row.full + row.part; ++j) {
+    u32x4 y = Type<R::T>::NINF;
+    if (units >> j & 1) {
+      const u32x4 u = row.load_tail(j);
+#pragma unroll
+      for (int e = 0; e < R::E; ++e)
+        if (stays(from_bits<R::T>(lift<R::T>(u, e)), row.id(j) + e)) lower<R::T>(y, e, lift<R::T>(u, e));
+    }
+    row.store(o, row.id(j), y);
+  }
   if (kept && threadIdx.x == 0) kept[blockIdx.x] = n;
 }
 
@@ -1085,7 +1098,7 @@ __global__ __launch_bounds__(R::LB) void k_filter_many(const void* logits, size_
       const bool write = out != logits;
       uint64_t all, above;
       uint32_t n = 0;
-      weigh<false>(
+      weigh<false, false>(
             row, sc, st, &all, &above, s, g,
             [&](int i, const u32x4& u, const float(&x)[R::E], const bool(&in)[R::E]) {
               if (!write) return;
@@ -1181,7 +1194,7 @@ __global__ __launch_bounds__(R::LB) void k_sample_many(const void* logits, size_
   const int w = threadIdx.x >> 6;
   bool exact = st.plan.low == INFINITY;
   if (!exact) {
-    weigh<false>(row, sc, st, &all, &above, s, g, nothing);
+    weigh<false, false>(row, sc, st, &all, &above, s, g, nothing);
     const int C = s.count;
     if (decide(row, sc, how, st, all, above, C, &k, s, g) && st.least <= st.plan.above.key) {
       const Keeps stays(k);
@@ -1201,7 +1214,10 @@ __global__ __launch_bounds__(R::LB) void k_sample_many(const void* logits, size_
     for (int i = threadIdx.x; i < CELLS; i += R::LB) s.cells[i] = 0;
     lds_barrier();
     const Start chosen{{KEY_NINF + 1, 0x7FFFFFFF}, KEY_NINF + 1, {k, INFINITY}};
-    weigh<true>(row, sc, chosen, &all, &above, s, g, nothing);
+    if (k.key == KEY_NINF + 1 && k.id >= V)
+      weigh<true, true>(row, sc, chosen, &all, &above, s, g, nothing);
+    else
+      weigh<true, false>(row, sc, chosen, &all, &above, s, g, nothing);
   }
   // the cell that holds the place
   const uint64_t h = (int)threadIdx.x < CELLS ? s.cells[threadIdx.x] : 0;
