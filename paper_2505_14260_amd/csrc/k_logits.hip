@@ -208,12 +208,14 @@ struct HeldRow<TYPE, LB, 0> : Row<TYPE, LB> {  // too long for that
 };
 
 // A row that is read once, of up to U whole tiles, AHEAD of them under way at a time, whose
-// units' largest stay in registers: they tell which few units to read again.
-template <int TYPE, int LB, int U, int AHEAD>
+// units' largest (of each PER of them) stay in registers: they tell which few units to read
+// again.
+template <int TYPE, int LB, int U, int AHEAD, int PER = 1>
 struct ToppedRow : Row<TYPE, LB> {
   using Row<TYPE, LB>::Row;
-  static constexpr int UNITS = U;
-  float top[U + 1];
+  static constexpr int UNITS = U, TOPS = U / PER;
+  static_assert(U % PER == 0 && U <= 64, "a bit for each unit");
+  float top[TOPS + 1];
   // m = f(unit) for every unit in order, m its largest.
   template <class F>
   MSD_DEV void read(F f) {
@@ -223,20 +225,22 @@ struct ToppedRow : Row<TYPE, LB> {
     if (this->part) last = this->load_tail(this->full);
 #pragma unroll
     for (int j = 0; j < U; ++j) {
-      top[j] = -INFINITY;
+      if (j % PER == 0) top[j / PER] = -INFINITY;
       if (j < this->full) {
         const u32x4 t = next[j % AHEAD];
         if (j + AHEAD < this->full) next[j % AHEAD] = this->load(j + AHEAD);
-        top[j] = f(t);
+        top[j / PER] = fmaxf(top[j / PER], f(t));
       }
     }
-    top[U] = this->part ? f(last) : -INFINITY;
+    top[TOPS] = this->part ? f(last) : -INFINITY;
   }
-  // The units that reach x.
+  // The units that may reach x (others may be among them, also past the row's end).
   MSD_DEV uint64_t reach(float x) const {
-    uint64_t m = this->part && top[U] >= x ? 1ull << this->full : 0;
+    uint64_t m = 0;
 #pragma unroll
-    for (int j = 0; j < U; ++j) m |= (uint64_t)(top[j] >= x) << j;
+    for (int j = 0; j < TOPS; ++j)
+      m |= (uint64_t)(top[j] >= x ? (1u << PER) - 1 : 0u) << (j * PER);
+    if (this->part && top[TOPS] >= x) m |= 1ull << this->full;
     return m;
   }
 };
@@ -552,14 +556,20 @@ MSD_DEV uint32_t min_key(float m, double min_d) {
   return k + ((double)of_key(k) < least);  // the next one up
 }
 
+// A unit's largest.
+template <class R>
+MSD_DEV float unit_max(const u32x4& u) {
+  float m = -INFINITY;
+#pragma unroll
+  for (int e = 0; e < R::E; ++e) m = fmaxf(m, from_bits<R::T>(lift<R::T>(u, e)));
+  return m;
+}
+
 // The key of the thread's largest.
 template <class R>
 MSD_DEV uint32_t thread_max(const R& row) {
   float m = -INFINITY;
-  row.template each<4>([&](int, int, const u32x4& u) {
-#pragma unroll
-    for (int e = 0; e < R::E; ++e) m = fmaxf(m, from_bits<R::T>(lift<R::T>(u, e)));
-  });
+  row.template each<4>([&](int, int, const u32x4& u) { m = fmaxf(m, unit_max<R>(u)); });
   return key_of(m);
 }
 
@@ -640,15 +650,6 @@ MSD_DEV void rank(FewLds& s, int C, int n, float m, float floor, Group<LB / 64>&
   lds_barrier();
 }
 
-// A unit's largest.
-template <class R>
-MSD_DEV float unit_max(const u32x4& u) {
-  float m = -INFINITY;
-#pragma unroll
-  for (int e = 0; e < R::E; ++e) m = fmaxf(m, from_bits<R::T>(lift<R::T>(u, e)));
-  return m;
-}
-
 // The first n (at most LOGITS_TOP_MAX and V) tokens of the row in order, in s.sorted:
 // those that reach a bound that n at least do, ranked.
 template <class R>
@@ -716,11 +717,12 @@ MSD_DEV int choose_few(const R& row, const Tops& t, const Scale& sc, const Logit
 // that surely stay, and it lists the tokens around the estimate, among which the border
 // then has to lie.  Where it does not (rows of very many equal logits), the border is
 // found digit by digit.
-constexpr int COUNTS = 4096, HEAD = 1024;
+constexpr int COUNTS = 4096, HEAD = 1024;   // (2^12 and 20 bits of a place are a word)
 constexpr double COUNTS_PER_T = 64;
 constexpr int PLACE_BITS = 40;              // of a bin's sum of places, in 2^-20
 constexpr int MANY = 4096;                  // the list: the border's bin and those beside it
 constexpr int BORDER = 512;                 // of those that share the border's bin of the list
+constexpr int LEVELS = 8 * (MANY + 2 * BORDER);
 constexpr int GROUP = 8;  // stretches of a wave that are summed together: a cell
 constexpr int CELLS = 256;  // a row's, 16 to a wave
 struct ManyLds : Lds {
@@ -728,8 +730,13 @@ struct ManyLds : Lds {
     uint64_t hist[BINS];
     uint64_t counts[COUNTS];
   };
-  uint64_t list[MANY];
-  uint64_t few[BORDER], few_w[BORDER];
+  union {
+    struct {
+      uint64_t list[MANY];
+      uint64_t few[BORDER], few_w[BORDER];
+    };
+    uint8_t levels[LEVELS];  // of the units, before there is a list
+  };
   uint64_t cells[CELLS];
 };
 
@@ -737,34 +744,39 @@ struct Bins {
   float ref, scale;
   MSD_DEV Bins(float r, double c)
       : ref(r), scale((float)fmin(c * (COUNTS_PER_T / M_LOG2E), 1e30)) {}
-  MSD_DEV float at(float x) const { return fmaf(x - ref, scale, (float)(COUNTS - HEAD)); }
+  // A bin and the place in it, in 2^-20; 0 for what lies below, and for a NaN.
+  MSD_DEV uint32_t at(float x) const {
+    const float b = fmaf(x - ref, scale * 0x1p20f, (float)(COUNTS - HEAD) * 0x1p20f);
+    return (uint32_t)fminf(fmaxf(b, 0.f), 0x1.fffffep31f);
+  }
   MSD_DEV float edge(float b) const { return ref + (b - (float)(COUNTS - HEAD)) / scale; }
+  // The coarse bin, of 256; it does not fall where x rises.
+  MSD_DEV uint32_t level(float x) const { return at(x) >> 24; }
 };
 
-// The row's largest, and with `count` its counts.
+// The row's largest, and with `count` its counts; with `levels` the level of each unit's
+// largest too.
 template <class R>
-MSD_DEV float largest(const R& row, double c, bool count, float* ref, ManyLds& s, Group<R::W>& g) {
+MSD_DEV float largest(const R& row, double c, bool count, bool levels, float* ref, ManyLds& s,
+                      Group<R::W>& g) {
   if (!count) return of_key(g.max(thread_max(row)));
   for (int i = threadIdx.x; i < COUNTS; i += R::LB) s.counts[i] = 0;
   float m = -INFINITY;
-  if (row.full || row.part) {
-    const u32x4 first = row.load_tail(0);
-#pragma unroll
-    for (int e = 0; e < R::E; ++e) m = fmaxf(m, from_bits<R::T>(lift<R::T>(first, e)));
-  }
+  if (row.full || row.part) m = unit_max<R>(row.load_tail(0));
   *ref = of_key(g.max(key_of(m)));  // (its barrier: the counts are clear)
   const Bins bins(*ref, c);
-  row.template each<4>([&](int, int, const u32x4& u) {
+  row.template each<4>([&](int j, int, const u32x4& u) {
+    float most = -INFINITY;
 #pragma unroll
     for (int e = 0; e < R::E; ++e) {
       const float x = from_bits<R::T>(lift<R::T>(u, e));
-      m = fmaxf(m, x);
-      const float b = bins.at(x);
-      const float bin = fminf(floorf(b), (float)(COUNTS - 1));
-      if (b >= 0.f)
-        atomicAdd((unsigned long long*)&s.counts[(int)bin],
-                  1ull << PLACE_BITS | (uint32_t)(fminf(b - bin, 1.f) * 0x1p20f));
+      most = fmaxf(most, x);
+      const uint32_t b = bins.at(x);
+      if (b)
+        atomicAdd((unsigned long long*)&s.counts[b >> 20], 1ull << PLACE_BITS | (b & 0xFFFFFu));
     }
+    m = fmaxf(m, most);
+    if (levels) s.levels[j * R::LB + threadIdx.x] = (uint8_t)bins.level(most);
   });
   return of_key(g.max(key_of(m)));
 }
@@ -795,7 +807,8 @@ MSD_DEV Plan estimate(float ref, const Scale& sc, const LogitsChoice& how, uint3
   if (least > KEY_NINF + 1) {
     // Does min_p end before top_p for certain?  Weights at the bins' edges, a hundredth
     // of a bin wider for the rounding of a place, bound those in them.
-    const float cut = fminf(bins.at(of_key(least)) - 1.f, (float)(COUNTS - 1));
+    const uint32_t at = bins.at(of_key(least));
+    const float cut = at ? (float)(at >> 20) - 1.f : -1.f;
     uint64_t most = 0, whole = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
@@ -1078,6 +1091,38 @@ __global__ __launch_bounds__(R::LB) void k_filter_few(const void* logits, size_t
   if (kept && threadIdx.x == 0) kept[blockIdx.x] = n;
 }
 
+// The same where the units' levels tell which of them to read.
+template <class R>
+MSD_DEV uint32_t put_leveled(const R& row, char* o, Kept k, const Bins& bins, const ManyLds& s) {
+  constexpr int AHEAD = 4;
+  const Keeps stays(k);
+  const uint32_t level = bins.level(stays.x);
+  const int units = row.full + row.part;
+  uint32_t n = 0;
+  for (int j0 = 0; j0 < units; j0 += AHEAD) {
+    u32x4 u[AHEAD];
+#pragma unroll
+    for (int b = 0; b < AHEAD; ++b) {
+      u[b] = Type<R::T>::NINF;
+      if (j0 + b < units && s.levels[(j0 + b) * R::LB + threadIdx.x] >= level)
+        u[b] = row.load_tail(j0 + b);
+    }
+#pragma unroll
+    for (int b = 0; b < AHEAD; ++b) {
+      if (j0 + b >= units) break;
+      const int i = row.id(j0 + b);
+#pragma unroll
+      for (int e = 0; e < R::E; ++e) {
+        const bool in = stays(from_bits<R::T>(lift<R::T>(u[b], e)), i + e);
+        if (!in) lower<R::T>(u[b], e, Type<R::T>::NINF & (R::T == MX_F32 ? ~0u : 0xFFFFu));
+        n += in;
+      }
+      row.store(o, i, u[b]);
+    }
+  }
+  return n;
+}
+
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_filter_many(const void* logits, size_t ld, int V,
                                                        LogitsChoice how, void* out, size_t ldo,
@@ -1087,12 +1132,16 @@ __global__ __launch_bounds__(R::LB) void k_filter_many(const void* logits, size_
   const R row(logits, ld, V);
   char* const o = static_cast<char*>(out) + (size_t)blockIdx.x * ldo * Type<R::T>::SIZE;
   float ref = 0.f;
-  const float m = largest(row, how.c, how.top_p < 1, &ref, s, g);
+  // min_p leaves few tokens, so that most units need not be read again
+  const bool levels = how.min_d > -INFINITY && row.per_wave() * R::LB <= LEVELS;
+  const float m = largest(row, how.c, how.top_p < 1 || levels, levels, &ref, s, g);
   Kept k{0xFF800000u, -1};  // nothing: +inf of no id
+  bool known = false;
   if (m > -INFINITY) {
     const Scale sc(m, how.c);
     const Start st = start_many(row, ref, sc, how, s, g);
     k = st.plan.above;
+    known = levels && fabsf(ref) < INFINITY && st.plan.low == INFINITY;
     if (st.plan.low < INFINITY) {
       // the pass writes as well, but in place, where the row may have to be read again
       const bool write = out != logits;
@@ -1129,7 +1178,8 @@ __global__ __launch_bounds__(R::LB) void k_filter_many(const void* logits, size_
       }
     }
   }
-  const uint64_t n = g.sum((uint64_t)put_filtered(row, o, k));
+  const uint64_t n = g.sum((uint64_t)(known ? put_leveled(row, o, k, Bins(ref, how.c), s)
+                                            : put_filtered(row, o, k)));
   if (kept && threadIdx.x == 0) kept[blockIdx.x] = (int)n;
 }
 
@@ -1184,7 +1234,7 @@ __global__ __launch_bounds__(R::LB) void k_sample_many(const void* logits, size_
   const R row(logits, ld, V);
   for (int i = threadIdx.x; i < CELLS; i += R::LB) s.cells[i] = 0;
   float ref = 0.f;
-  const float m = largest(row, how.c, how.top_p < 1, &ref, s, g);
+  const float m = largest(row, how.c, how.top_p < 1, false, &ref, s, g);
   if (!(m > -INFINITY)) return put_no_token(tokens, logprobs, keep);
   const Scale sc(m, how.c);
   const Start st = start_many(row, ref, sc, how, s, g);
@@ -1480,7 +1530,9 @@ void by_tops(int rows, int cols, F f) {
   if (rows > 256 && holds<LongTwo>(cols)) return f(Tag<LongTwo>());
   if (holds<One>(cols)) return f(Tag<One>());
   if (holds<LongOne>(cols)) return f(Tag<LongOne>());
-  f(Tag<ToppedRow<TYPE, 1024, MOST, 6>>());
+  if constexpr (MOST > 38)
+    if (holds<ToppedRow<TYPE, 1024, 38, 10>>(cols)) return f(Tag<ToppedRow<TYPE, 1024, 38, 10>>());
+  f(Tag<ToppedRow<TYPE, 1024, MOST, MOST / 8, MOST / 32>>());
 }
 
 template <int TYPE, class F>
