@@ -234,12 +234,13 @@ struct ToppedRow : Row<TYPE, LB> {
     }
     top[TOPS] = this->part ? f(last) : -INFINITY;
   }
-  // The units that may reach x (others may be among them, also past the row's end).
+  // The units that may reach x (others may be among them).
   MSD_DEV uint64_t reach(float x) const {
     uint64_t m = 0;
 #pragma unroll
     for (int j = 0; j < TOPS; ++j)
       m |= (uint64_t)(top[j] >= x ? (1u << PER) - 1 : 0u) << (j * PER);
+    if (this->full < 64) m &= (1ull << this->full) - 1;
     if (this->part && top[TOPS] >= x) m |= 1ull << this->full;
     return m;
   }
@@ -576,22 +577,28 @@ MSD_DEV uint32_t thread_max(const R& row) {
 // ----------------------------------------------------------- a few first tokens ----
 
 constexpr int FEW = 1024;      // tokens that are ranked among each other,
-constexpr int FEW_PAIRS = 128; // up to so many by comparing all
+constexpr int FEW_PAIRS = 128; // up to so many by comparing all,
+constexpr int BUCKETS = 2048;  // more of them within buckets
 struct FewLds : Lds {
   union {
     uint64_t hist[BINS];
-    uint32_t base[FEW + 1];
+    uint32_t base[BUCKETS + 1];
     uint64_t weights[LOGITS_TOP_MAX];
   };
   uint64_t list[FEW], other[FEW];
   uint64_t sorted[LOGITS_TOP_MAX];
 };
 
-// s.list[0 .. C) ranked: its first n in s.sorted.  m: the row's largest, floor at most the
-// smallest value of the list.  More than a few are first brought into buckets of
-// their value, then compared within those.
+// The bucket of a key at or below that of the row's largest: 32 to a factor of two of the
+// distance between the keys.  It does not fall where the key does.
+MSD_DEV int bucket_of(uint32_t most, uint32_t key) {
+  return (int)((__float_as_uint((float)(most - key)) >> 18) - (most == key ? 0 : (126u << 5)));
+}
+static_assert(((127 + 32) << 5) - (126 << 5) < BUCKETS, "the largest distance");
+
+// s.list[0 .. C) ranked: its first n in s.sorted.  most: the key of the row's largest.
 template <int LB>
-MSD_DEV void rank(FewLds& s, int C, int n, float m, float floor, Group<LB / 64>& g) {
+MSD_DEV void rank(FewLds& s, int C, int n, uint32_t most, Group<LB / 64>& g) {
   if (C <= FEW_PAIRS) {
     if ((int)threadIdx.x < C) {
       const uint64_t me = s.list[threadIdx.x];
@@ -602,46 +609,40 @@ MSD_DEV void rank(FewLds& s, int C, int n, float m, float floor, Group<LB / 64>&
     lds_barrier();
     return;
   }
-  constexpr int PER = FEW / LB;
-  const float width = (m - floor) * (1.f / (FEW - 1));
-  const float c = width > 0 && width < INFINITY ? 1.f / width : 0.f;  // (c = inf: as good as 0)
-  const auto bucket = [&](uint64_t place) {
-    const float d = (m - of_key((uint32_t)(place >> 32))) * c;
-    return d > 0 ? (int)fminf(d, (float)(FEW - 1)) : 0;
-  };
-  for (int i = threadIdx.x; i <= FEW; i += LB) s.base[i] = 0;
+  constexpr int PER = FEW / LB, WIDE = BUCKETS / LB;
+  for (int i = threadIdx.x; i <= BUCKETS; i += LB) s.base[i] = 0;
   lds_barrier();
   uint64_t mine[PER];
-  int at[PER];
+  int at[PER], bucket[PER];
 #pragma unroll
   for (int q = 0; q < PER; ++q) {
     const int i = threadIdx.x + q * LB;
     if (i >= C) continue;
     mine[q] = s.list[i];
-    at[q] = (int)atomicAdd(&s.base[bucket(mine[q])], 1u);
+    bucket[q] = bucket_of(most, (uint32_t)(mine[q] >> 32));
+    at[q] = (int)atomicAdd(&s.base[bucket[q]], 1u);
   }
   lds_barrier();
-  uint32_t size[PER], sum = 0;
+  uint32_t size[WIDE], sum = 0;
 #pragma unroll
-  for (int q = 0; q < PER; ++q) sum += size[q] = s.base[threadIdx.x * PER + q];
+  for (int q = 0; q < WIDE; ++q) sum += size[q] = s.base[threadIdx.x * WIDE + q];
   uint64_t all;
   uint32_t run = (uint32_t)g.before(sum, &all);
 #pragma unroll
-  for (int q = 0; q < PER; ++q) {
-    s.base[threadIdx.x * PER + q] = run;
+  for (int q = 0; q < WIDE; ++q) {
+    s.base[threadIdx.x * WIDE + q] = run;
     run += size[q];
   }
-  if (threadIdx.x == LB - 1) s.base[FEW] = run;
+  if (threadIdx.x == LB - 1) s.base[BUCKETS] = run;
   lds_barrier();
 #pragma unroll
   for (int q = 0; q < PER; ++q)
-    if ((int)threadIdx.x + q * LB < C) s.other[s.base[bucket(mine[q])] + at[q]] = mine[q];
+    if ((int)threadIdx.x + q * LB < C) s.other[s.base[bucket[q]] + at[q]] = mine[q];
   lds_barrier();
 #pragma unroll
   for (int q = 0; q < PER; ++q) {
     if ((int)threadIdx.x + q * LB >= C) continue;
-    const int b = bucket(mine[q]);
-    const int from = s.base[b], to = s.base[b + 1];
+    const int from = s.base[bucket[q]], to = s.base[bucket[q] + 1];
     int above = from;
     if (above >= n) continue;
     for (int k = from; k < to; ++k) above += s.other[k] > mine[q];
@@ -677,7 +678,7 @@ MSD_DEV void first_tokens(const R& row, const Tops& t, int n, FewLds& s, Group<R
     lds_barrier();
     C = s.count;
   }
-  rank<R::LB>(s, C, n, of_key(t.max), at_least, g);
+  rank<R::LB>(s, C, n, t.max, g);
 }
 
 // The tokens that stay of a few at most (0 < top_k <= LOGITS_TOP_MAX): their number, in
@@ -1517,7 +1518,7 @@ void by_held(int rows, int cols, F f) {
 
 // The same of rows that keep their units' largest.
 template <int TYPE, class F>
-void by_tops(int rows, int cols, F f) {
+void by_tops(int rows, int cols, int k, F f) {
   constexpr int MOST = LOGITS_MAX_COLS / (1024 * Type<TYPE>::E);
   using Short = ToppedRow<TYPE, 256, 8, 8>;
   // rows that share a CU hide each other's reading; a row alone has all of it under way
@@ -1525,7 +1526,8 @@ void by_tops(int rows, int cols, F f) {
   using LongTwo = ToppedRow<TYPE, 512, 38, 6>;
   using One = ToppedRow<TYPE, 1024, 8, 8>;
   using LongOne = ToppedRow<TYPE, 1024, 18, 18>;
-  if (cols * Type<TYPE>::SIZE <= SHORT_ROW) return f(Tag<Short>());
+  // (more than a quarter of the threads' largest bound too long a list)
+  if (cols * Type<TYPE>::SIZE <= SHORT_ROW && k <= 64) return f(Tag<Short>());
   if (rows > 256 && holds<Two>(cols)) return f(Tag<Two>());
   if (rows > 256 && holds<LongTwo>(cols)) return f(Tag<LongTwo>());
   if (holds<One>(cols)) return f(Tag<One>());
@@ -1551,7 +1553,7 @@ void launch_logits_top(const void* x, int type, size_t ld, int rows, int cols, i
                        int* ids, float* lse, hipStream_t st) {
   if (rows <= 0) return;
   by_type(type, [&](auto t) {
-    by_tops<t()>(rows, cols, [&](auto r) {
+    by_tops<t()>(rows, cols, k, [&](auto r) {
       using R = typename decltype(r)::type;
       k_top<R><<<rows, R::LB, 0, st>>>(x, ld, cols, k, values, ids, lse);
     });
@@ -1565,7 +1567,7 @@ void launch_logits_sample(const void* x, int type, size_t ld, int rows, int cols
   const bool few = how.top_k > 0 && how.top_k <= LOGITS_TOP_MAX;
   by_type(type, [&](auto t) {
     if (few)
-      by_tops<t()>(rows, cols, [&](auto r) {
+      by_tops<t()>(rows, cols, how.top_k, [&](auto r) {
         using R = typename decltype(r)::type;
         k_sample_few<R><<<rows, R::LB, 0, st>>>(x, ld, cols, how, uniforms, tokens, logprobs, keep);
       });
@@ -1584,7 +1586,7 @@ void launch_logits_filter(const void* x, int type, size_t ld, int rows, int cols
   const bool few = how.top_k > 0 && how.top_k <= LOGITS_TOP_MAX;
   by_type(type, [&](auto t) {
     if (few)
-      by_tops<t()>(rows, cols, [&](auto r) {
+      by_tops<t()>(rows, cols, how.top_k, [&](auto r) {
         using R = typename decltype(r)::type;
         k_filter_few<R><<<rows, R::LB, 0, st>>>(x, ld, cols, how, out, ldo, kept);
       });
