@@ -718,22 +718,25 @@ MSD_DEV int choose_few(const R& row, const Tops& t, const Scale& sc, const Logit
 // that surely stay, and it lists the tokens around the estimate, among which the border
 // then has to lie.  Where it does not (rows of very many equal logits), the border is
 // found digit by digit.
-constexpr int COUNTS = 4096, HEAD = 1024;   // (2^12 and 20 bits of a place are a word)
 constexpr double COUNTS_PER_T = 64;
-constexpr int PLACE_BITS = 40;              // of a bin's sum of places, in 2^-20
-constexpr int MANY = 4096;                  // the list: the border's bin and those beside it
-constexpr int BORDER = 512;                 // of those that share the border's bin of the list
-constexpr int LEVELS = 8 * (MANY + 2 * BORDER);
-constexpr int GROUP = 8;  // stretches of a wave that are summed together: a cell
+constexpr int PLACE_BITS = 40;  // of a bin's sum of places, in 2^-20
+constexpr int GROUP = 8;    // stretches of a wave that are summed together: a cell
 constexpr int CELLS = 256;  // a row's, 16 to a wave
+// Short rows take less, so that more of them share a CU.
+template <int LB>
 struct ManyLds : Lds {
+  // a bin and 20 bits of a place in it are a word
+  static constexpr int COUNTS = LB == 256 ? 2048 : 4096, HEAD = COUNTS / 4;
+  static constexpr int LIST = LB == 256 ? 1024 : 4096;   // tokens around the estimate
+  static constexpr int BORDER = LB == 256 ? 256 : 512;   // that share the border's bin of those
+  static constexpr int LEVELS = 8 * (LIST + 2 * BORDER);
   union {
     uint64_t hist[BINS];
     uint64_t counts[COUNTS];
   };
   union {
     struct {
-      uint64_t list[MANY];
+      uint64_t list[LIST];
       uint64_t few[BORDER], few_w[BORDER];
     };
     uint8_t levels[LEVELS];  // of the units, before there is a list
@@ -741,31 +744,33 @@ struct ManyLds : Lds {
   uint64_t cells[CELLS];
 };
 
+template <int LB>
 struct Bins {
+  static constexpr int COUNTS = ManyLds<LB>::COUNTS, HEAD = ManyLds<LB>::HEAD;
   float ref, scale;
   MSD_DEV Bins(float r, double c)
       : ref(r), scale((float)fmin(c * (COUNTS_PER_T / M_LOG2E), 1e30)) {}
   // A bin and the place in it, in 2^-20; 0 for what lies below, and for a NaN.
   MSD_DEV uint32_t at(float x) const {
     const float b = fmaf(x - ref, scale * 0x1p20f, (float)(COUNTS - HEAD) * 0x1p20f);
-    return (uint32_t)fminf(fmaxf(b, 0.f), 0x1.fffffep31f);
+    return (uint32_t)fminf(fmaxf(b, 0.f), (float)COUNTS * (0x1p20f - 0x1p-4f));
   }
   MSD_DEV float edge(float b) const { return ref + (b - (float)(COUNTS - HEAD)) / scale; }
-  // The coarse bin, of 256; it does not fall where x rises.
+  // The coarse bin, of 256 at most; it does not fall where x rises.
   MSD_DEV uint32_t level(float x) const { return at(x) >> 24; }
 };
 
 // The row's largest, and with `count` its counts; with `levels` the level of each unit's
 // largest too.
 template <class R>
-MSD_DEV float largest(const R& row, double c, bool count, bool levels, float* ref, ManyLds& s,
+MSD_DEV float largest(const R& row, double c, bool count, bool levels, float* ref, ManyLds<R::LB>& s,
                       Group<R::W>& g) {
   if (!count) return of_key(g.max(thread_max(row)));
-  for (int i = threadIdx.x; i < COUNTS; i += R::LB) s.counts[i] = 0;
+  for (int i = threadIdx.x; i < s.COUNTS; i += R::LB) s.counts[i] = 0;
   float m = -INFINITY;
   if (row.full || row.part) m = unit_max<R>(row.load_tail(0));
   *ref = of_key(g.max(key_of(m)));  // (its barrier: the counts are clear)
-  const Bins bins(*ref, c);
+  const Bins<R::LB> bins(*ref, c);
   row.template each<4>([&](int j, int, const u32x4& u) {
     float most = -INFINITY;
 #pragma unroll
@@ -792,9 +797,9 @@ struct Plan {
 // The estimate from the counts, bins from the last down.  least: the key that min_p asks for.
 template <class R>
 MSD_DEV Plan estimate(float ref, const Scale& sc, const LogitsChoice& how, uint32_t least,
-                      ManyLds& s, Group<R::W>& g) {
-  constexpr int PER = COUNTS / R::LB;
-  const Bins bins(ref, sc.c);
+                      ManyLds<R::LB>& s, Group<R::W>& g) {
+  constexpr int COUNTS = ManyLds<R::LB>::COUNTS, PER = COUNTS / R::LB;
+  const Bins<R::LB> bins(ref, sc.c);
   uint32_t n[PER];
   uint64_t w[PER], sum = 0, all;
 #pragma unroll
@@ -851,7 +856,7 @@ MSD_DEV Plan estimate(float ref, const Scale& sc, const LogitsChoice& how, uint3
 // The last token that stays by top-p, of which `want` of the weight is among the C listed;
 // false where it is not, or where too many are alike.
 template <int LB>
-MSD_DEV bool border(ManyLds& s, int C, const Plan& p, uint64_t want, const Scale& sc, Kept* k,
+MSD_DEV bool border(ManyLds<LB>& s, int C, const Plan& p, uint64_t want, const Scale& sc, Kept* k,
                     Group<LB / 64>& g) {
   const float high = fminf(of_key(p.above.key), sc.m);
   const float width = high - p.low;
@@ -875,14 +880,14 @@ MSD_DEV bool border(ManyLds& s, int C, const Plan& p, uint64_t want, const Scale
     const float x = of_key((uint32_t)(s.list[i] >> 32));
     if (bin_of(x) != bin) continue;
     const int at = atomicAdd(&s.count, 1);
-    if (at < BORDER) {
+    if (at < s.BORDER) {
       s.few[at] = s.list[i];
       s.few_w[at] = weight(x, sc);
     }
   }
   lds_barrier();
   const int n = s.count;
-  if (n > BORDER) return false;
+  if (n > s.BORDER) return false;
   for (int i = threadIdx.x; i < n; i += LB) {
     const uint64_t me = s.few[i];
     uint64_t before = 0;
@@ -902,7 +907,7 @@ struct Start {
 };
 template <class R>
 MSD_DEV Start start_many(const R& row, float ref, const Scale& sc, const LogitsChoice& how,
-                         ManyLds& s, Group<R::W>& g) {
+                         ManyLds<R::LB>& s, Group<R::W>& g) {
   const R& mem = row;
   constexpr int LAST = 0x7FFFFFFF;
   Start st{{KEY_NINF + 1, LAST}, KEY_NINF + 1, {{0xFF800000u, -1}, 3.402823466e38f}};
@@ -943,7 +948,7 @@ MSD_DEV Start start_many(const R& row, float ref, const Scale& sc, const LogitsC
 // each unit.
 template <bool EXACT, bool ALL, class R, class F>
 MSD_DEV void weigh(const R& row, const Scale& sc, const Start& st, uint64_t* all, uint64_t* above,
-                   ManyLds& s, Group<R::W>& g, F f) {
+                   ManyLds<R::LB>& s, Group<R::W>& g, F f) {
   const Keeps stays(st.plan.above), within(st.limit);
   const float low = st.plan.low;
   const bool limited = !EXACT && st.limit.key > KEY_NINF + 1;
@@ -1003,7 +1008,7 @@ MSD_DEV void weigh(const R& row, const Scale& sc, const Start& st, uint64_t* all
     for (; marked; marked &= marked - 1) {
       const int j0 = (__ffsll((unsigned long long)marked) - 1) << pairs;
       for (int j = j0; j <= j0 + pairs && j < row.full + row.part; ++j)
-        append(row, row.id(j), row.load_tail(j), s.list, MANY, s, [&](float v, int id) {
+        append(row, row.id(j), row.load_tail(j), s.list, s.LIST, s, [&](float v, int id) {
           return v >= low && !(v >= stays.x) && (!limited || within(v, id));
         });
     }
@@ -1016,10 +1021,10 @@ MSD_DEV void weigh(const R& row, const Scale& sc, const Start& st, uint64_t* all
 // in passes of their own.
 template <class R>
 MSD_DEV bool decide(const R& row, const Scale& sc, const LogitsChoice& how, const Start& st,
-                    uint64_t all, uint64_t above, int C, Kept* k, ManyLds& s, Group<R::W>& g) {
+                    uint64_t all, uint64_t above, int C, Kept* k, ManyLds<R::LB>& s, Group<R::W>& g) {
   uint64_t want = (uint64_t)ceil((double)all * how.top_p);
   want = want < 1 ? 1 : want > all ? all : want;
-  const bool found = C <= MANY && want > above &&
+  const bool found = C <= s.LIST && want > above &&
                      border<R::LB>(s, C, st.plan, want - above, sc, k, g);
   if (!found) *k = shortest(row, &sc, want, s.hist, g);
   if (st.least > k->key) *k = {st.least, 0x7FFFFFFF};
@@ -1094,7 +1099,7 @@ __global__ __launch_bounds__(R::LB) void k_filter_few(const void* logits, size_t
 
 // The same where the units' levels tell which of them to read.
 template <class R>
-MSD_DEV uint32_t put_leveled(const R& row, char* o, Kept k, const Bins& bins, const ManyLds& s) {
+MSD_DEV uint32_t put_leveled(const R& row, char* o, Kept k, const Bins<R::LB>& bins, const ManyLds<R::LB>& s) {
   constexpr int AHEAD = 4;
   const Keeps stays(k);
   const uint32_t level = bins.level(stays.x);
@@ -1128,13 +1133,13 @@ template <class R>
 __global__ __launch_bounds__(R::LB) void k_filter_many(const void* logits, size_t ld, int V,
                                                        LogitsChoice how, void* out, size_t ldo,
                                                        int* kept) {
-  __shared__ ManyLds s;
+  __shared__ ManyLds<R::LB> s;
   Group<R::W> g{s};
   const R row(logits, ld, V);
   char* const o = static_cast<char*>(out) + (size_t)blockIdx.x * ldo * Type<R::T>::SIZE;
   float ref = 0.f;
   // min_p leaves few tokens, so that most units need not be read again
-  const bool levels = how.min_d > -INFINITY && row.per_wave() * R::LB <= LEVELS;
+  const bool levels = how.min_d > -INFINITY && row.per_wave() * R::LB <= s.LEVELS;
   const float m = largest(row, how.c, how.top_p < 1 || levels, levels, &ref, s, g);
   Kept k{0xFF800000u, -1};  // nothing: +inf of no id
   bool known = false;
@@ -1179,7 +1184,7 @@ __global__ __launch_bounds__(R::LB) void k_filter_many(const void* logits, size_
       }
     }
   }
-  const uint64_t n = g.sum((uint64_t)(known ? put_leveled(row, o, k, Bins(ref, how.c), s)
+  const uint64_t n = g.sum((uint64_t)(known ? put_leveled(row, o, k, Bins<R::LB>(ref, how.c), s)
                                             : put_filtered(row, o, k)));
   if (kept && threadIdx.x == 0) kept[blockIdx.x] = (int)n;
 }
@@ -1229,7 +1234,7 @@ template <class R>
 __global__ __launch_bounds__(R::LB) void k_sample_many(const void* logits, size_t ld, int V,
                                                        LogitsChoice how, const float* uniforms,
                                                        int* tokens, float* logprobs, bool keep) {
-  __shared__ ManyLds s;
+  __shared__ ManyLds<R::LB> s;
   Group<R::W> g{s};
   const float u = uniforms[blockIdx.x];
   const R row(logits, ld, V);
