@@ -46,12 +46,6 @@ MSD_DEV float from_bits(uint32_t h) {
   return __half2float(__builtin_bit_cast(__half, (uint16_t)h));
 }
 template <int TYPE>
-MSD_DEV uint32_t to_bits(float v) {
-  if constexpr (TYPE == MX_F32) return __float_as_uint(v);
-  if constexpr (TYPE == MX_BF16) return f2bf(v);
-  return __builtin_bit_cast(uint16_t, __float2half(v));
-}
-template <int TYPE>
 MSD_DEV uint32_t bits_at(const char* p, int i) {
   if constexpr (TYPE == MX_F32) return reinterpret_cast<const uint32_t*>(p)[i];
   return reinterpret_cast<const uint16_t*>(p)[i];
@@ -276,8 +270,9 @@ struct Scale {
   }
 };
 // With 128 added, as a double: sums of n such bits are n times 128's more than the sum.
-MSD_DEV uint64_t bits_of(float x, const Scale& s) {
-  const double t = fmax(((double)x - s.m64) * s.c, -64.0);  // (a NaN too)
+// d: x - m.
+MSD_DEV uint64_t bits_at_distance(double d, const Scale& s) {
+  const double t = fmax(d * s.c, -64.0);  // (a NaN too)
   const double k = t + 0x1.8p52;                          // rounded in its last bits
   const double r = t - (k - 0x1.8p52);
   double q = 0x1.b63880a30e9ffp-24;
@@ -295,6 +290,9 @@ MSD_DEV uint64_t bits_of(float x, const Scale& s) {
   return (uint64_t)__double_as_longlong(w + 128.0);
 }
 constexpr uint64_t BITS_128 = 0x4060000000000000ull;
+MSD_DEV uint64_t bits_of(float x, const Scale& s) {
+  return bits_at_distance((double)x - s.m64, s);
+}
 MSD_DEV uint64_t weight(float x, const Scale& s) { return bits_of(s(x), s) - BITS_128; }
 
 // ------------------------------------------------------- waves and workgroups ----
@@ -428,12 +426,10 @@ struct Keeps {  // the same as values
 
 // ------------------------------------------------------------------ thresholds ----
 
-// The bin of hist in which the running sum reaches `want` (of *all, for the whole, when
-// `share` of it is wanted), with the sum before it and its own in s.found.  Bins ascend
-// from bin 0 on, or descend from the last.
+// The bin of hist in which the running sum reaches `want`, with the sum before it and its
+// own in s.found; *all: the whole sum.  Bins ascend from bin 0 on, or descend from the last.
 template <int W, bool DOWN>
-MSD_DEV uint64_t find_bin(const uint64_t* hist, uint64_t want, double share, uint64_t* all,
-                          Group<W>& g) {
+MSD_DEV void find_bin(const uint64_t* hist, uint64_t want, uint64_t* all, Group<W>& g) {
   constexpr int PER = BINS / (W * 64);
   uint64_t h[PER], sum = 0;
 #pragma unroll
@@ -442,10 +438,6 @@ MSD_DEV uint64_t find_bin(const uint64_t* hist, uint64_t want, double share, uin
     sum += h[i] = hist[DOWN ? BINS - 1 - b : b];
   }
   uint64_t run = g.before(sum, all);
-  if (share > 0) {
-    want = (uint64_t)ceil((double)*all * share);
-    want = want < 1 ? 1 : want > *all ? *all : want;
-  }
   if (run < want && want <= run + sum) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
@@ -459,7 +451,6 @@ MSD_DEV uint64_t find_bin(const uint64_t* hist, uint64_t want, double share, uin
     }
   }
   lds_barrier();
-  return want;
 }
 
 template <int W>
@@ -494,7 +485,7 @@ MSD_DEV Kept shortest(const R& row, const Scale* sc, uint64_t want, uint64_t* hi
       }
     });
     lds_barrier();
-    find_bin<R::W, true>(hist, want, 0, &all, g);
+    find_bin<R::W, true>(hist, want, &all, g);
     prefix |= (uint32_t)s.bin << low;
     want -= s.found[0];
     ties = s.found[1];
@@ -652,21 +643,21 @@ MSD_DEV void rank(FewLds& s, int C, int n, uint32_t most, Group<LB / 64>& g) {
 }
 
 // The first n (at most LOGITS_TOP_MAX and V) tokens of the row in order, in s.sorted:
-// those that reach a bound that n at least do, ranked.
-template <class R>
-MSD_DEV void first_tokens(const R& row, const Tops& t, int n, FewLds& s, Group<R::W>& g) {
-  const bool all = t.floor <= KEY_NINF;
-  const float at_least = all ? -INFINITY : of_key(t.floor);
+// those that reach a bound that n at least do, ranked; with DEAD also those of -inf, if the
+// others do not suffice.  Returns their number.
+template <bool DEAD, class R>
+MSD_DEV int first_tokens(const R& row, const Tops& t, int n, FewLds& s, Group<R::W>& g) {
+  const float at_least = of_key(max(t.floor, KEY_NINF + 1));
   const Row<R::T, R::LB>& mem = row;
   uint64_t units = row.reach(at_least);
   for (; units; units &= units - 1) {
     const int j = __ffsll((unsigned long long)units) - 1;
     append(mem, mem.id(j), mem.load_tail(j), s.list, FEW, s,
-           [&](float x, int) { return x >= at_least || all; });
+           [&](float x, int) { return x >= at_least; });
   }
   lds_barrier();
   int C = s.count;
-  if (C > FEW) {  // very many equal ones, or the largest in few threads
+  if (C > FEW || (DEAD && C < n)) {  // very many equal ones, or the largest in few threads
     const Kept k = shortest(mem, nullptr, n, s.hist, g);
     clear_count(s);
     mem.template each<2>([&](int, int i, const u32x4& u) {
@@ -678,7 +669,9 @@ MSD_DEV void first_tokens(const R& row, const Tops& t, int n, FewLds& s, Group<R
     lds_barrier();
     C = s.count;
   }
+  n = min(n, C);
   rank<R::LB>(s, C, n, t.max, g);
+  return n;
 }
 
 // The tokens that stay of a few at most (0 < top_k <= LOGITS_TOP_MAX): their number, in
@@ -686,8 +679,7 @@ MSD_DEV void first_tokens(const R& row, const Tops& t, int n, FewLds& s, Group<R
 template <class R>
 MSD_DEV int choose_few(const R& row, const Tops& t, const Scale& sc, const LogitsChoice& how,
                        uint64_t* all, FewLds& s, Group<R::W>& g) {
-  const int n = min(how.top_k, row.V);
-  first_tokens(row, t, n, s, g);
+  const int n = first_tokens<false>(row, t, min(how.top_k, row.V), s, g);
   uint32_t key = 0;
   uint64_t w = 0;
   if ((int)threadIdx.x < n) {
@@ -756,35 +748,45 @@ struct Bins {
     return (uint32_t)fminf(fmaxf(b, 0.f), (float)COUNTS * (0x1p20f - 0x1p-4f));
   }
   MSD_DEV float edge(float b) const { return ref + (b - (float)(COUNTS - HEAD)) / scale; }
+  // The weight there, of the row's largest at most; not rounded to a logit.
+  MSD_DEV uint64_t weight_at(float b, const Scale& s) const {
+    const double d = (double)ref - s.m64 + (double)(b - (float)(COUNTS - HEAD)) / (double)scale;
+    return bits_at_distance(fmin(d, 0.0), s) - BITS_128;
+  }
   // The coarse bin, of 256 at most; it does not fall where x rises.
   MSD_DEV uint32_t level(float x) const { return at(x) >> 24; }
 };
 
 // The row's largest, and with `count` its counts; with `levels` the level of each unit's
-// largest too.
+// largest too.  Where the row's largest is past the last bin (low temperatures, rows whose
+// waves' first are masked) the row is counted again around that one.
 template <class R>
 MSD_DEV float largest(const R& row, double c, bool count, bool levels, float* ref, ManyLds<R::LB>& s,
                       Group<R::W>& g) {
   if (!count) return of_key(g.max(thread_max(row)));
-  for (int i = threadIdx.x; i < s.COUNTS; i += R::LB) s.counts[i] = 0;
-  float m = -INFINITY;
-  if (row.full || row.part) m = unit_max<R>(row.load_tail(0));
-  *ref = of_key(g.max(key_of(m)));  // (its barrier: the counts are clear)
-  const Bins<R::LB> bins(*ref, c);
-  row.template each<4>([&](int j, int, const u32x4& u) {
-    float most = -INFINITY;
+  float m = row.full || row.part ? unit_max<R>(row.load_tail(0)) : -INFINITY;
+#pragma unroll 1
+  for (int round = 0;; ++round) {
+    for (int i = threadIdx.x; i < s.COUNTS; i += R::LB) s.counts[i] = 0;
+    *ref = of_key(g.max(key_of(m)));  // (its barrier: the counts are clear)
+    const Bins<R::LB> bins(*ref, c);
+    row.template each<4>([&](int j, int, const u32x4& u) {
+      float most = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < R::E; ++e) {
-      const float x = from_bits<R::T>(lift<R::T>(u, e));
-      most = fmaxf(most, x);
-      const uint32_t b = bins.at(x);
-      if (b)
-        atomicAdd((unsigned long long*)&s.counts[b >> 20], 1ull << PLACE_BITS | (b & 0xFFFFFu));
-    }
-    m = fmaxf(m, most);
-    if (levels) s.levels[j * R::LB + threadIdx.x] = (uint8_t)bins.level(most);
-  });
-  return of_key(g.max(key_of(m)));
+      for (int e = 0; e < R::E; ++e) {
+        const float x = from_bits<R::T>(lift<R::T>(u, e));
+        most = fmaxf(most, x);
+        const uint32_t b = bins.at(x);
+        if (b)
+          atomicAdd((unsigned long long*)&s.counts[b >> 20], 1ull << PLACE_BITS | (b & 0xFFFFFu));
+      }
+      m = fmaxf(m, most);
+      if (levels) s.levels[j * R::LB + threadIdx.x] = (uint8_t)bins.level(most);
+    });
+    m = of_key(g.max(key_of(m)));
+    if (round || !(fabsf(m) < INFINITY) || bins.at(m) >> 20 < (uint32_t)s.COUNTS - 1) return m;
+    lds_barrier();  // before the counts are cleared
+  }
 }
 
 // What is known before the weights: tokens that surely stay, and the least of the others
@@ -807,8 +809,8 @@ MSD_DEV Plan estimate(float ref, const Scale& sc, const LogitsChoice& how, uint3
     const int b = COUNTS - 1 - (threadIdx.x * PER + i);
     const uint64_t places = s.counts[b] & ((1ull << PLACE_BITS) - 1);
     n[i] = (uint32_t)(s.counts[b] >> PLACE_BITS);
-    const float mean = (float)b + (float)places * 0x1p-20f / (float)n[i];  // (0 / 0: of none)
-    sum += w[i] = n[i] * weight(fminf(bins.edge(mean), sc.m), sc);
+    const float mean = (float)b + (float)places * 0x1p-20f / (float)n[i];
+    sum += w[i] = n[i] ? n[i] * bins.weight_at(mean, sc) : 0;
   }
   if (least > KEY_NINF + 1) {
     // Does min_p end before top_p for certain?  Weights at the bins' edges, a hundredth
@@ -819,13 +821,18 @@ MSD_DEV Plan estimate(float ref, const Scale& sc, const LogitsChoice& how, uint3
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const float b = (float)(COUNTS - 1 - (threadIdx.x * PER + i));
-      whole += n[i] * weight(fminf(bins.edge(b - 0.01f), sc.m), sc);
-      if (b >= cut) most += n[i] * weight(b < COUNTS - 1 ? fminf(bins.edge(b + 1.01f), sc.m) : sc.m, sc);
+      whole += n[i] * bins.weight_at(b - 0.01f, sc);
+      if (b >= cut) most += n[i] * bins.weight_at(b < COUNTS - 1 ? b + 1.01f : 2.f * COUNTS, sc);
     }
     most = g.sum(most);
     whole = g.sum(whole);
     if (cut >= 0.f && (double)most < (double)whole * how.top_p * (1 - 0x1p-20))
       return {{least, 0x7FFFFFFF}, INFINITY};
+  }
+  if (threadIdx.x == 0) {  // where no weight is to be seen
+    s.bin = COUNTS - 1;
+    s.count = 0;
+    s.found[0] = 0;
   }
   uint64_t run = g.before(sum, &all);
   const uint64_t want = (uint64_t)((double)all * how.top_p);
@@ -850,6 +857,8 @@ MSD_DEV Plan estimate(float ref, const Scale& sc, const LogitsChoice& how, uint3
   const float high = bins.edge(at + around);
   Plan p{{0xFF800000u, -1}, bins.edge(at - around)};
   if (at + around < (float)COUNTS && high < sc.m) p.above = {key_of(high), 0x7FFFFFFF};
+  // (temperatures whose bins no float tells apart: nothing is listed)
+  if (!(fabsf(p.low) < INFINITY) || !(p.low < high)) p = {{0xFF800000u, -1}, 3.402823466e38f};
   return p;
 }
 
@@ -872,7 +881,7 @@ MSD_DEV bool border(ManyLds<LB>& s, int C, const Plan& p, uint64_t want, const S
   }
   lds_barrier();
   uint64_t all;
-  find_bin<LB / 64, false>(s.hist, want, 0, &all, g);
+  find_bin<LB / 64, false>(s.hist, want, &all, g);
   if (want < 1 || want > all) return false;
   const int bin = s.bin;
   want -= s.found[0];
@@ -1171,6 +1180,7 @@ __global__ __launch_bounds__(R::LB) void k_filter_many(const void* logits, size_
           (k.key < st.plan.above.key || (k.key == st.plan.above.key && k.id >= st.plan.above.id))) {
         // of those that may stay, the ones that do not
         const Keeps stays(k);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the row's stores are done
         __syncthreads();
         for (int i = threadIdx.x; i < C; i += R::LB) {
           const int id = (int)~(uint32_t)s.list[i];
@@ -1356,7 +1366,7 @@ __global__ __launch_bounds__(R::LB) void k_top(const void* logits, size_t ld, in
     if (threadIdx.x == 0)
       lse[blockIdx.x] = fabsf(m) < INFINITY ? (float)((double)m + log(sum)) : m;
   }
-  first_tokens(row, t, n, s, g);
+  first_tokens<true>(row, t, n, s, g);
   if ((int)threadIdx.x < n) {
     const size_t o = (size_t)blockIdx.x * n + threadIdx.x;
     const uint64_t top = s.sorted[threadIdx.x];

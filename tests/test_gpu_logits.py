@@ -218,6 +218,62 @@ def test_stay_special_rows(how):
         check_choice(x, u, how)
 
 
+@pytest.mark.parametrize("dead", ["-inf", "lowest"])
+@pytest.mark.parametrize("how", [
+    dict(), dict(top_k=30), dict(top_k=400), dict(top_p=0.8), dict(min_p=0.1),
+    dict(top_p=0.9, min_p=0.01), dict(temperature=0.05, top_p=0.9), dict(temperature=40.0, top_p=0.5),
+    dict(top_k=200, top_p=0.7)], ids=str)
+def test_stay_masked_rows(how, dead):
+    """A mask leaves a few tokens, anywhere: also where a row's first are masked."""
+    for cols in (300, 5000, 40000, 152064):
+        print(f"case: {cols} columns", flush=True)
+        g = gen(cols)
+        for type_ in ("f32", "bf16"):
+            low = float("-inf") if dead == "-inf" else torch.finfo(TYPES[type_]).min
+            x = torch.full((7, cols), low)
+            for r, live in enumerate((1, 2, 20, 60, 250, 280, 300)):
+                at = torch.randperm(cols, generator=g)[:live]
+                x[r, at] = torch.randn(live, generator=g) * 3 + r
+            x[5, : cols // 2] = low
+            x[6, cols // 3:] = low
+            check_choice(x.to(TYPES[type_]), torch.rand(7, generator=g), how)
+
+
+def test_stay_with_a_late_maximum_and_odd_scales():
+    """The largest far above what a row begins with, in units of the temperature; logits far
+    from 0; temperatures at which all weigh alike."""
+    for cols in (3000, 70000):
+        g = gen(cols)
+        x = torch.randn(8, cols, generator=g)
+        x[0, cols - 1] = 30
+        x[1, cols // 2:] += 25
+        x[2] += 3000
+        x[3] = x[3] * 1e-3 - 5e4
+        x[4] *= 1e30
+        x[5, cols - 5:] = torch.tensor([50.0, 49.9, 49.8, 49.7, 49.6])
+        x[6] = torch.linspace(-80, 80, cols)
+        x[7] = torch.linspace(80, -80, cols)
+        u = torch.rand(8, generator=g)
+        for how in (dict(temperature=0.02, top_p=0.9), dict(temperature=0.3, top_p=0.95, min_p=0.01),
+                    dict(temperature=1.0, top_p=0.99), dict(temperature=1e-5, top_p=0.6),
+                    dict(temperature=1e9, top_p=0.3), dict(temperature=1e45, top_p=0.75),
+                    dict(temperature=2.0, min_p=0.3), dict(temperature=0.01, top_k=300, top_p=0.9)):
+            print(f"case: {cols} columns, {how}", flush=True)
+            check_choice(x, u, how)
+
+
+def test_top_of_masked_rows():
+    for cols in (300, 5000, 60000):
+        x = torch.full((5, cols), float("-inf"))
+        for r, live in enumerate((1, 9, 100, 255, 299)):
+            at = torch.randperm(cols, generator=gen(r))[:live]
+            x[r, at] = torch.randn(live, generator=gen(r + 9))
+        for k in (1, 64, 100, 256):
+            print(f"case: {cols} columns, k {k}", flush=True)
+            check_top(x.cuda(), k)
+            check_top(torch.where(x == float("-inf"), torch.finfo(torch.float32).min, x).cuda(), k)
+
+
 def test_stay_with_exact_borders():
     """Weights that are powers of two sum exactly: a border may lie on a sum."""
     log2 = float(np.log(2.0))
