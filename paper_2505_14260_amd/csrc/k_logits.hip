@@ -921,11 +921,10 @@ MSD_DEV Start start_many(const R& row, float ref, const Scale& sc, const LogitsC
   constexpr int LAST = 0x7FFFFFFF;
   Start st{{KEY_NINF + 1, LAST}, KEY_NINF + 1, {{0xFF800000u, -1}, 3.402823466e38f}};
   if (how.min_d > -INFINITY) st.least = min_key(sc.m, how.min_d);
-  bool limited = false;
-  if (how.top_k > 0 && how.top_k < row.V) {
+  const bool limited = how.top_k > 0 && how.top_k < row.V;
+  if (limited) {  // (the counts are gone then)
     const Kept f = shortest(mem, nullptr, how.top_k, s.hist, g);
-    limited = f.key > KEY_NINF;
-    if (limited) st.limit = f;
+    if (f.key > KEY_NINF) st.limit = f;
   }
   if (how.top_p == 1) {
     st.plan = {st.limit, INFINITY};

@@ -262,6 +262,20 @@ def test_stay_with_a_late_maximum_and_odd_scales():
             check_choice(x, u, how)
 
 
+def test_stay_with_a_top_k_of_more_than_a_mask_leaves():
+    for cols, live in ((3000, 700), (40000, 2500)):
+        g = gen(cols)
+        x = torch.full((6, cols), float("-inf"))
+        for r in range(6):
+            at = torch.randperm(cols, generator=g)[:live + r]
+            x[r, at] = torch.randn(live + r, generator=g) * (0.02 if r & 1 else 2) + r
+        u = torch.rand(6, generator=g)
+        for how in (dict(top_k=live + 90, top_p=0.9, min_p=0.5), dict(top_k=live + 90, top_p=0.5, min_p=0.1),
+                    dict(top_k=live + 90, top_p=0.3, min_p=0.97), dict(top_k=live + 1, top_p=0.95)):
+            print(f"case: {cols} columns, {how}", flush=True)
+            check_choice(x, u, how)
+
+
 def test_top_of_masked_rows():
     for cols in (300, 5000, 60000):
         x = torch.full((5, cols), float("-inf"))
