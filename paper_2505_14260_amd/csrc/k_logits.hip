@@ -8,9 +8,14 @@
 //
 // Weights exp((x - max) / T) decide which token lies next to a border, so they are
 // computed in 64 bits and held as whole numbers of 2^-45: 2^18 of them sum exactly, in
-// any order, atomics included.
+// any order, atomics included: no result depends on the order of the atomics.
 //
-// One workgroup a row.
+// One workgroup a row; no memory but the operands and the workgroup's own LDS, so calls on
+// several streams and captured graphs share nothing.  Offsets of a row are 64-bit, within a
+// row 32-bit (at most 2^18 logits).
+//
+// Times here are of one MI355X, on which a copy of 82 MB reads and writes 7.0 TB/s, one of
+// 2 GiB 5.0 TB/s, and the smallest launch takes 4.2 us in a row of launches.
 #include <hip/hip_fp16.h>
 
 #include <type_traits>
@@ -162,6 +167,9 @@ struct Row {
     }
     if (part) f(full, id(full), last);
   }
+  // Past the caches: a row's outputs are not read again by this call, and in the caches they
+  // would push out rows that are (gradients of 639 x 32,000 f32 52 -> 44 us, of 1,151 x
+  // 152,064 bf16 319 -> 288; filter of 488 x 152,064 f32 190 -> 178).
   MSD_DEV void store(char* o, int i, const u32x4& u) const {
     if (i + E <= V) {
       __builtin_nontemporal_store(u, reinterpret_cast<unit*>(o + (size_t)i * Type<TYPE>::SIZE));
@@ -173,7 +181,8 @@ struct Row {
   }
 };
 
-// The same with up to U whole tiles and the last one in registers.
+// The same with up to U whole tiles and the last one in registers: for a second pass that
+// needs every logit again (the gradient), HBM is read once.
 template <int TYPE, int LB, int U>
 struct HeldRow : Row<TYPE, LB> {
   static constexpr int UNITS = U;
@@ -203,7 +212,8 @@ struct HeldRow<TYPE, LB, 0> : Row<TYPE, LB> {  // too long for that
 
 // A row that is read once, of up to U whole tiles, AHEAD of them under way at a time, whose
 // units' largest (of each PER of them) stay in registers: they tell which few units to read
-// again.
+// again.  A quarter of a held row's registers or less, so that long rows share a CU too (top
+// 128 of 1,151 x 152,064 bf16 161 us held, 114 so).
 template <int TYPE, int LB, int U, int AHEAD, int PER = 1>
 struct ToppedRow : Row<TYPE, LB> {
   using Row<TYPE, LB>::Row;
@@ -269,6 +279,8 @@ struct Scale {
     return finite ? x : x == INFINITY ? 0.f : -INFINITY;
   }
 };
+// About 25 vector instructions, of 64 bits at the rate of 32-bit ones here (0.59 ns for a
+// wave's on one CU); the library's exp takes more, and its last bits are not a contract.
 // With 128 added, as a double: sums of n such bits are n times 128's more than the sum.
 // d: x - m.
 MSD_DEV uint64_t bits_at_distance(double d, const Scale& s) {
@@ -389,8 +401,9 @@ struct Group {
   }
 };
 
-// The key of a row's largest, and one that the r largest of the threads' largest reach
-// in every wave: so W r tokens at least reach it, and few more of most rows.
+// A bound for a row's n first tokens without a search over the row: the key of its largest,
+// and one that the r largest of the threads' largest reach in every wave: so W r tokens at
+// least reach it, and few more of most rows.
 struct Tops {
   uint32_t max, floor;
 };
@@ -567,9 +580,8 @@ MSD_DEV uint32_t thread_max(const R& row) {
 
 // ----------------------------------------------------------- a few first tokens ----
 
-constexpr int FEW = 1024;      // tokens that are ranked among each other,
-constexpr int FEW_PAIRS = 128; // up to so many by comparing all,
-constexpr int BUCKETS = 2048;  // more of them within buckets
+constexpr int FEW = 1024;      // tokens that are ranked,
+constexpr int BUCKETS = 2048;  // among those of their bucket
 struct FewLds : Lds {
   union {
     uint64_t hist[BINS];
@@ -587,19 +599,13 @@ MSD_DEV int bucket_of(uint32_t most, uint32_t key) {
 }
 static_assert(((127 + 32) << 5) - (126 << 5) < BUCKETS, "the largest distance");
 
-// s.list[0 .. C) ranked: its first n in s.sorted.  most: the key of the row's largest.
+// s.list[0 .. C) ranked: its first n in s.sorted.  most: the key of the row's largest.  A
+// token is compared with those of its bucket only: of short lists no slower than all pairs
+// (top 10 of a row of 32,000 8.0 us, by pairs 8.8; top 64 of 61 of them 10.3 and 10.7; top 20
+// of 640 rows of 8,192 11.2 and 10.4), of long ones much faster (top 28 of one row of 304,
+// which lists all of it, 9.7 and 40).
 template <int LB>
 MSD_DEV void rank(FewLds& s, int C, int n, uint32_t most, Group<LB / 64>& g) {
-  if (C <= FEW_PAIRS) {
-    if ((int)threadIdx.x < C) {
-      const uint64_t me = s.list[threadIdx.x];
-      int above = 0;
-      for (int k = 0; k < C; ++k) above += s.list[k] > me;
-      if (above < n) s.sorted[above] = me;
-    }
-    lds_barrier();
-    return;
-  }
   constexpr int PER = FEW / LB, WIDE = BUCKETS / LB;
   for (int i = threadIdx.x; i <= BUCKETS; i += LB) s.base[i] = 0;
   lds_barrier();
@@ -709,12 +715,14 @@ MSD_DEV int choose_few(const R& row, const Tops& t, const Scale& sc, const Logit
 // to a few tokens.  The next pass computes the weights: those of all for their sum, those
 // that surely stay, and it lists the tokens around the estimate, among which the border
 // then has to lie.  Where it does not (rows of very many equal logits), the border is
-// found digit by digit.
+// found digit by digit.  Sample by top_p of 512 x 152,064 f32: 355 us with every weight in
+// a histogram of 64-bit sums, 228 with the border estimated from counts, 158 with the means.
 constexpr double COUNTS_PER_T = 64;
 constexpr int PLACE_BITS = 40;  // of a bin's sum of places, in 2^-20
 constexpr int GROUP = 8;    // stretches of a wave that are summed together: a cell
 constexpr int CELLS = 256;  // a row's, 16 to a wave
-// Short rows take less, so that more of them share a CU.
+// Short rows take 31 KB for 76 KB, so that five share a CU and not two: sample of 3,136 x
+// 300 f32 100 -> 45 us, filter of 3,000 x 5,000 bf16 119 -> 62.
 template <int LB>
 struct ManyLds : Lds {
   // a bin and 20 bits of a place in it are a word
@@ -1059,7 +1067,7 @@ MSD_DEV uint32_t put_filtered(const R& row, char* o, Kept k) {
   return n;
 }
 
-// The row's first reading for a few first tokens.
+// The row's first reading for a few first tokens: its largest and its threads', no weights.
 template <class R>
 MSD_DEV Tops read_tops(R& row, int n, Group<R::W>& g) {
   float mine = -INFINITY;
@@ -1071,6 +1079,9 @@ MSD_DEV Tops read_tops(R& row, int n, Group<R::W>& g) {
   return tops(key_of(mine), (min(n, row.V) + R::W - 1) / R::W, g);
 }
 
+// Filter with a small top_k: one reading of the row, its writing, and the units with one of
+// the tokens read again.  Bound by HBM: 488 x 152,064 f32, top_k 50, 593 MB in 120 us, 4.9
+// TB/s, the rate of a large copy (133 us with every unit read again).
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_filter_few(const void* logits, size_t ld, int V,
                                                       LogitsChoice how, void* out, size_t ldo,
@@ -1105,7 +1116,9 @@ __global__ __launch_bounds__(R::LB) void k_filter_few(const void* logits, size_t
   if (kept && threadIdx.x == 0) kept[blockIdx.x] = n;
 }
 
-// The same where the units' levels tell which of them to read.
+// The same where the units' levels tell which of them to read: under min_p most hold no
+// token that stays, so that the row is read once (filter of 488 x 152,064 f32, min_p 0.02:
+// 177 us with every unit read again, 162 with levels).
 template <class R>
 MSD_DEV uint32_t put_leveled(const R& row, char* o, Kept k, const Bins<R::LB>& bins, const ManyLds<R::LB>& s) {
   constexpr int AHEAD = 4;
@@ -1137,6 +1150,13 @@ MSD_DEV uint32_t put_leveled(const R& row, char* o, Kept k, const Bins<R::LB>& b
   return n;
 }
 
+// Filter with any number of tokens that stay: a pass that counts, one that weighs and (where
+// the output is not the input) writes all that may stay, and the few near the border masked
+// in it.  Many rows are bound by HBM and by the weights' arithmetic, which the two rows of a
+// CU overlap in part: 488 x 152,064 f32, min_p 0.02 and top_p 0.98, 164 us, 3.6 TB/s of what
+// has to move (119 us at a copy's rate); 27 x 32,000 f32 25 us, of one CU's arithmetic on a
+// row (at the instructions' rates 7 us of weights and 2 of counts) and the chain of barriers
+// between them.
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_filter_many(const void* logits, size_t ld, int V,
                                                        LogitsChoice how, void* out, size_t ldo,
@@ -1215,6 +1235,9 @@ MSD_DEV void put_no_token(int* tokens, float* logprobs, bool keep) {
   if (logprobs) logprobs[blockIdx.x] = -INFINITY;
 }
 
+// Sample with a small top_k: as the filter's, and the draw among the ranked tokens in the
+// order of their ids.  One row on a CU takes the latency of its chain and what one CU reads:
+// 64 x 152,064 bf16, top_k 50, 16 us for 304 KB a CU.
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_sample_few(const void* logits, size_t ld, int V,
                                                       LogitsChoice how, const float* uniforms,
@@ -1239,6 +1262,15 @@ __global__ __launch_bounds__(R::LB) void k_sample_few(const void* logits, size_t
     put_token((int)~me, of_key((uint32_t)(s.sorted[threadIdx.x] >> 32)), all, sc, tokens, logprobs);
 }
 
+// Sample with any number of tokens that stay: a pass that counts, one that weighs, and the
+// sums of 2,048 or 4,096 neighbouring ids (a cell) tell where to read again for the draw;
+// without top_p a pass for the largest and one for the weights.  Rows are in runs, not in
+// tiles, so that a wave's cell is of neighbouring ids.  Bound by the arithmetic of the
+// weights with the first pass's HBM time not hidden by it: 512 x 152,064 f32, top_p 0.95, 148
+// us (62 us for its bytes once at a copy's rate; about 70 us for 78 million weights on 256
+// CUs at the instructions' rates).  A row alone: 1 x 32,000 f32 without a choice 13 us.
+//   Few rows take one CU each all the same (8 x 152,064 f32, top_p: 71 us); a row over several
+// workgroups would need memory of the caller's and two more launches or a grid's barrier.
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_sample_many(const void* logits, size_t ld, int V,
                                                        LogitsChoice how, const float* uniforms,
@@ -1348,6 +1380,11 @@ MSD_DEV double row_sum(const Online& o, float m, float c, Group<W>& g) {
   return g.sum(o.sum == 0.f ? 0.0 : (double)(o.sum * exp_of(o.m, m, c)));
 }
 
+// Top: one reading of the row, with its log-sum-exp (32-bit sums a thread, 64-bit over the
+// row), and the ranking.  Many rows are bound by HBM: 1,151 x 152,064 bf16, k 128, 350 MB in
+// 105 us, 3.3 TB/s, two rows to a CU, of which the ranking of one hides behind the reading of
+// the other in part; 639 x 32,000 f32, k 64, 82 MB in 23 us.  Few rows by the chain: 61 x
+// 50,021 f16, k 200, 15 us; 1 x 32,000 f32 8 us.
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_top(const void* logits, size_t ld, int V, int n,
                                                float* values, int* ids, float* lse) {
@@ -1408,6 +1445,15 @@ struct Chains {
   int head[1024];
 };
 
+// Distillation, loss and gradient in one pass or either alone: the loss is
+//   sum q (log q - log p) = sum q (log q - (x - m) / T + log sum e^((x - m) / T)),
+// so it takes the row's sum and the entries' logits only; the gradient g / T (p - q) is p's
+// for every column and q's at the entries, which the thread that writes their unit takes
+// off before it rounds: no second write, no atomics on the output.  Sums and weights in 32
+// bits within a thread, in 64 over the row; the gradient recomputes its sum, since a row is
+// held anyway.  Bound by HBM: 639 x 32,000 f32 164 MB in 43 us (3.8 TB/s: 639 rows are 512
+// and a tail of 127), 1,151 x 152,064 bf16 700 MB in 173 us (4.0 TB/s: a row to a CU, whose
+// registers it fills, 4.5 rounds), the loss alone 65 us (5.4 TB/s).
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_distill(const void* logits, size_t ld, int V,
                                                    LogitsTeacher t, float* loss, float* lse,
@@ -1506,7 +1552,11 @@ struct Tag {
   using type = R;
 };
 
-// Rows of up to this many bytes take a workgroup of 256 threads.
+// Rows of up to this many bytes take a workgroup of 256 threads: several share a CU, and a
+// row has as few barriers' waits.  Against 1024 threads, us: top 64 of 3,000 x 1,000 f32 20
+// (89) and of 3,000 x 8,192 32 (79), filter by top_p 41 (133) and 82 (180), sample by top_p
+// of 3,000 x 1,000 47 (157), gradients 23 (109) and 43 (122).  Of 61 rows of 8,192: top 8.9
+// (9.3), filter 18.4 (17.0), gradient 14.3 (12.6).
 constexpr int SHORT_ROW = 256 * 8 * 16;
 
 template <class R>
@@ -1515,8 +1565,10 @@ bool holds(int cols) {
 }
 
 // Calls f with the type for a row of `cols` that is held: by 256 threads if it is short; by
-// 512, two rows to a CU, where there are more rows than CUs; by 1024; or read from memory
-// in every pass.
+// 512, two rows to a CU, where there are more rows than CUs (639 x 32,000 f32 43 us, by 1024
+// 50); by 1024; or read from memory in every pass, where no registers hold it.  A long row
+// of 18 units that is read twice instead of held is no slower (1,151 x 152,064 bf16, 250 us
+// for 248 in two calls) but reads half as much again.
 template <int TYPE, class F>
 void by_held(int rows, int cols, F f) {
   using Short = HeldRow<TYPE, 256, 8>;
@@ -1530,7 +1582,9 @@ void by_held(int rows, int cols, F f) {
   f(Tag<HeldRow<TYPE, 1024, 0>>());
 }
 
-// The same of rows that keep their units' largest.
+// The same of rows that keep their units' largest.  512 threads against 1024 where there are
+// more rows than CUs: 639 x 32,000 f32 24.9 us (31.5), 300 x 32,000 16.4 (20.5), 1,151 x
+// 152,064 bf16 115 (119).
 template <int TYPE, class F>
 void by_tops(int rows, int cols, int k, F f) {
   constexpr int MOST = LOGITS_MAX_COLS / (1024 * Type<TYPE>::E);
@@ -1540,7 +1594,8 @@ void by_tops(int rows, int cols, int k, F f) {
   using LongTwo = ToppedRow<TYPE, 512, 38, 6>;
   using One = ToppedRow<TYPE, 1024, 8, 8>;
   using LongOne = ToppedRow<TYPE, 1024, 18, 18>;
-  // (more than a quarter of the threads' largest bound too long a list)
+  // (more than a quarter of the threads' largest bound too long a list: top 250 of 26 x
+  // 15,400 bf16 takes 62 us with 256 threads, 14 with 1024)
   if (cols * Type<TYPE>::SIZE <= SHORT_ROW && k <= 64) return f(Tag<Short>());
   if (rows > 256 && holds<Two>(cols)) return f(Tag<Two>());
   if (rows > 256 && holds<LongTwo>(cols)) return f(Tag<LongTwo>());
@@ -1551,6 +1606,9 @@ void by_tops(int rows, int cols, int k, F f) {
   f(Tag<ToppedRow<TYPE, 1024, MOST, MOST / 8, MOST / 32>>());
 }
 
+// The same of rows that take any number of tokens: 512 threads against 1024 where there are
+// more rows than CUs: sample by top_p of 640 x 32,000 f32 71 us (95), of 512 x 152,064 158
+// (174); filter of 488 x 152,064 165 (157).
 template <int TYPE, class F>
 void by_runs(int rows, int cols, F f) {
   if (cols * Type<TYPE>::SIZE <= SHORT_ROW)
@@ -1621,7 +1679,8 @@ void launch_logits_distill(const void* x, int type, size_t ld, int rows, int col
       using R = typename decltype(r)::type;
       k_distill<R><<<rows, R::LB, 0, st>>>(x, ld, cols, t_, loss, lse, grad, dx, ldd);
     };
-    // without a gradient a row is read once, and need not be held
+    // without a gradient a row is read once, and need not be held (1,151 x 152,064 bf16 65
+    // us; both calls of the pair 246, with 1024 threads and held rows 288)
     if (!dx && rows > 256 && cols * Type<t()>::SIZE > SHORT_ROW)
       run(Tag<HeldRow<t(), 512, 0>>());
     else
