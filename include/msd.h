@@ -339,7 +339,8 @@ int msd_accept_compact(msd_ctx* ctx, int n_seq, const int32_t* seqs_h,
  * probability p(x) / (1 - target mass of the children already rejected
  * there), where p = softmax(logits / temperature) at the current node; a
  * rejection removes x from p.  When no child is accepted, the bonus token is
- * drawn from p without the rejected tokens.  The emitted tokens follow the
+ * drawn from p without the rejected tokens (where that leaves none with a logit above
+ * -inf, it is the last rejected one that has mass).  The emitted tokens follow the
  * target's own sampling distribution.
  *
  * logits_d [n_seq][n_nodes][V] float32: the logits msd_verify wrote for these

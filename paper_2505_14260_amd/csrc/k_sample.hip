@@ -217,6 +217,11 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_accept_sample(
         bi = sh_bi[i];
       }
     y = bi < V ? bi : 0;
+    // Where that is masked out, all that stays was rejected: 1 - removed exceeds what the
+    // last of them has by the roundings of the sum, so that the last is drawn.
+    if (bv == -INFINITY)
+      for (int i = 0; i < n_rej; ++i)
+        if (scaled(lg, sh_rej[i], inv_t) != -INFINITY) y = sh_rej[i];
   }
   for (int j = threadIdx.x; j < MSD_MAX_TREE; j += SAMPLE_THREADS) {
     const int u = j < n ? sh_path[j] : -1;

@@ -117,6 +117,43 @@ def test_filtered_acceptance_matches_oracle(setup):
             assert np.isfinite(flt[node, token])
 
 
+def test_a_rejection_of_all_that_stays_emits_one_of_it(setup):
+    """Two tokens stay and both are drafted.  In 32 bits 1 - p(first) can be more than
+    p(second), so that the second may be rejected too, though all the mass left is its."""
+    from oracle import sampling as S
+    from paper_2505_14260_amd.msd import msd_seq_len
+    wl, eng, m, prompt, spec = setup
+    T = spec.n_nodes + 1
+    print("case: both of the tokens that stay rejected", flush=True)
+    trees = eng.new_trees(1)
+    eng.prefill(0, *prompt)
+    eng.draft_tree([0], spec, trees)
+    _, logits = eng.verify([0], trees, T, want_logits=True)
+    L = msd_seq_len(eng.ctx, 0)
+    tree = eng.trees_to_host(trees, 1)[0]
+    a, b = [int(tree.token[u]) for u in range(1, T) if tree.parent[u] == 0][:2]
+    lg = torch.full((T, wl.dims.vocab), float("-inf"))
+    lg[0, a] = 0.0
+    lg[0, b] = math.log(0.55 * 2.0 ** -23)  # p(first) rounds to 1 - 2^-23
+    seed = None
+    for base in range(0, 1 << 28, 1 << 22):
+        with np.errstate(over="ignore"):
+            def uniform(j, seeds):
+                z = seeds + np.uint64((S.draw_index(0, L, j) + 1) * S._GAMMA & S._M64)
+                z = (z ^ z >> np.uint64(30)) * np.uint64(0xBF58476D1CE4E5B9)
+                z = (z ^ z >> np.uint64(27)) * np.uint64(0x94D049BB133111EB)
+                return (z ^ z >> np.uint64(31)) >> np.uint64(40)
+            seeds = np.arange(base, base + (1 << 22), dtype=np.uint64)
+            seeds = seeds[uniform(0, seeds) >= (1 << 24) - 2]
+            seeds = seeds[uniform(1, seeds) >= 0.6 * (1 << 24)]
+        if len(seeds):
+            seed = int(seeds[0])
+            break
+    assert S.draw_uniform(seed, 0, L, 0) >= 1 - 2.0 ** -23 and S.draw_uniform(seed, 0, L, 1) >= 0.6
+    em, _ = eng.accept_sample([0], trees, T, lg.cuda(), 1.0, seed)
+    assert [int(x) for x in em[0]] == [b]
+
+
 def test_settings_are_refused(setup):
     from paper_2505_14260_amd.msd import MSDError, Sampling
     wl, eng, m, prompt, spec = setup
