@@ -1448,12 +1448,13 @@ struct Chains {
 // Distillation, loss and gradient in one pass or either alone: the loss is
 //   sum q (log q - log p) = sum q (log q - (x - m) / T + log sum e^((x - m) / T)),
 // so it takes the row's sum and the entries' logits only; the gradient g / T (p - q) is p's
-// for every column and q's at the entries, which the thread that writes their unit takes
-// off before it rounds: no second write, no atomics on the output.  Sums and weights in 32
-// bits within a thread, in 64 over the row (a weight below 2^-126 of the largest is 0); the
-// gradient recomputes its sum, since a row is held anyway.  Bound by HBM: 639 x 32,000 f32 164 MB in 43 us (3.8 TB/s: 639 rows are 512
-// and a tail of 127), 1,151 x 152,064 bf16 700 MB in 173 us (4.0 TB/s: a row to a CU, whose
-// registers it fills, 4.5 rounds), the loss alone 65 us (5.4 TB/s).
+// for every column and q's at the entries, which the thread that writes their unit takes off
+// before it rounds: no second write, no atomics on the output.  Sums and weights in 32 bits
+// within a thread, in 64 over the row (a weight below 2^-126 of the largest is 0); the
+// gradient recomputes its sum, since a row is held anyway.  Bound by HBM: 639 x 32,000 f32
+// 164 MB in 43 us (3.8 TB/s: 639 rows are 512 and a tail of 127), 1,151 x 152,064 bf16 700
+// MB in 173 us (4.0 TB/s: a row to a CU, whose registers it fills, 4.5 rounds), the loss
+// alone 65 us (5.4 TB/s).
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_distill(const void* logits, size_t ld, int V,
                                                    LogitsTeacher t, float* loss, float* lse,
