@@ -918,15 +918,18 @@ MSD_DEV bool border(ManyLds<LB>& s, int C, const Plan& p, uint64_t want, const S
 
 // What of a row's choice does not need its weights.
 struct Start {
-  Kept limit;      // of top_k
+  static constexpr int LAST = 0x7FFFFFFF;
+  Kept limit;      // of top_k; without one the least token above -inf, with id LAST
   uint32_t least;  // of min_p
   Plan plan;
+  // (the id tells: the k-th token itself may be the least one)
+  MSD_DEV bool limited() const { return limit.id != LAST; }
 };
 template <class R>
 MSD_DEV Start start_many(const R& row, float ref, const Scale& sc, const LogitsChoice& how,
                          ManyLds<R::LB>& s, Group<R::W>& g) {
   const R& mem = row;
-  constexpr int LAST = 0x7FFFFFFF;
+  constexpr int LAST = Start::LAST;
   Start st{{KEY_NINF + 1, LAST}, KEY_NINF + 1, {{0xFF800000u, -1}, 3.402823466e38f}};
   if (how.min_d > -INFINITY) st.least = min_key(sc.m, how.min_d);
   const bool limited = how.top_k > 0 && how.top_k < row.V;
@@ -967,7 +970,7 @@ MSD_DEV void weigh(const R& row, const Scale& sc, const Start& st, uint64_t* all
                    ManyLds<R::LB>& s, Group<R::W>& g, F f) {
   const Keeps stays(st.plan.above), within(st.limit);
   const float low = st.plan.low;
-  const bool limited = !EXACT && st.limit.key > KEY_NINF + 1;
+  const bool limited = !EXACT && st.limited();
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   uint64_t sum_all = 0, sum_above = 0, cell = 0, marked = 0;
   const int pairs = row.per_wave() > 64;  // a mark is of two units
@@ -1310,7 +1313,7 @@ __global__ __launch_bounds__(R::LB) void k_sample_many(const void* logits, size_
   if (exact) {
     for (int i = threadIdx.x; i < CELLS; i += R::LB) s.cells[i] = 0;
     lds_barrier();
-    const Start chosen{{KEY_NINF + 1, 0x7FFFFFFF}, KEY_NINF + 1, {k, INFINITY}};
+    const Start chosen{{KEY_NINF + 1, Start::LAST}, KEY_NINF + 1, {k, INFINITY}};
     if (k.key == KEY_NINF + 1 && k.id >= V)
       weigh<true, true>(row, sc, chosen, &all, &above, s, g, nothing);
     else
