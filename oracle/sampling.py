@@ -15,7 +15,8 @@ q = delta_x the acceptance probability is p(x) and the adjusted distribution
 is p with x removed and renormalised.  Children are tried in node order (rank
 order); each rejection removes its token from p before the next child is
 tried, and after the last rejection the bonus token is drawn from what is
-left.  Walking down from the root, an accepted child becomes the node whose
+left (where roundings rejected all that has mass, it is the last of that).
+Walking down from the root, an accepted child becomes the node whose
 children are tried next, with the target distribution at that child.  The
 emitted tokens are then distributed exactly as plain sampling from the target
 (checked by the tests).
@@ -107,10 +108,13 @@ def sample_accept(tree, logits, temperature, seed, seq, L):
             lo = cdf[y - 1] if y > 0 else 0.0
             margin = min(target - lo, cdf[y] - target) / total
         else:
-            # every remaining token has zero mass: the best remaining logit
+            # every remaining token has zero mass: the best remaining logit, or, where
+            # none is above -inf, the last rejected token whose logit is
             masked = np.asarray(logits[cur], dtype=np.float64).copy()
             masked[rejected] = -np.inf
             y = int(np.argmax(masked))
+            if masked[y] == -np.inf:
+                y = next((x for x in reversed(rejected) if logits[cur][x] > -np.inf), y)
             margin = 0.0
         decisions.append({"kind": "bonus", "at": cur, "r": r, "token": y, "margin": margin})
         emitted = [int(tree.token[u]) for u in path[1:]] + [y]
