@@ -585,9 +585,11 @@ int msd_logits_filter(const void* logits_d, int type, size_t ld, int rows, int c
  * loss_d, lse_d and the pair grad_d, dlogits_d may each be NULL, not all; grad_d and
  * dlogits_d go together.  loss and gradient come in one pass over the logits when both
  * are asked for.  A row without entries (or with values of -inf only) has loss 0 and
- * gradient 0.  Where the teacher has mass and the student's logit is -inf the loss is
- * infinite (the gradient is not).  A NaN, or an infinite value other than -inf, makes
- * its row NaN; so does a student's row of -inf.
+ * gradient 0, whatever its logits.  In other rows, where the teacher has mass and the
+ * student's logit is -inf the loss is infinite (the gradient is not); a NaN, or an
+ * infinite value other than -inf, on either side makes loss and gradient NaN, and so
+ * does a student's row of -inf.  lse is of the logits alone: NaN for a NaN or +inf among
+ * them, -inf for a row of -inf.
  */
 int msd_logits_distill(const void* logits_d, int type, size_t ld, int rows, int cols,
                        const msd_teacher* teacher, float* loss_d, float* lse_d,

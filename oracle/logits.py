@@ -82,7 +82,7 @@ def distill(row, ids, values, temperature, grad=1.0):
     ids, t = ids[here], t[here]
     with np.errstate(invalid="ignore", divide="ignore"):
         m = np.max(x)
-        lse = m + np.log(np.exp(x - m).sum())
+        lse = m + np.log(np.exp(x - m).sum()) if m != -np.inf else m
         p = np.exp(x - lse)
         q = np.zeros(len(x))
         if not len(t) or np.max(t) == -np.inf:
