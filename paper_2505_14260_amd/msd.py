@@ -519,9 +519,11 @@ class Engine:
         ids, values, temperature = teacher
         for t, dtype, what in ((ids, torch.int32, "ids"), (values, torch.float32, "values")):
             if t.dtype != dtype or t.dim() != 2 or t.shape[0] != len(tokens) - 1 \
-                    or t.shape != ids.shape or not t.is_contiguous() or not t.is_cuda:
+                    or t.shape != ids.shape or not t.is_contiguous() \
+                    or t.device != self.torch_stream.device:
                 raise ValueError(f"teacher's {what}: wants contiguous {dtype} of {len(tokens) - 1} "
-                                 f"rows on the GPU, got {t.dtype} {tuple(t.shape)} on {t.device}")
+                                 f"rows on {self.torch_stream.device}, got {t.dtype} "
+                                 f"{tuple(t.shape)} on {t.device}")
         self.torch_stream.wait_stream(torch.cuda.current_stream(self.dev))
         return msd_train_accumulate_top(
             self.ctx, seq, tokens, is_visual, ptr,
