@@ -77,6 +77,11 @@ class Sampling(ctypes.Structure):
     _fields_ = [("temperature", ctypes.c_double), ("top_p", ctypes.c_double),
                 ("min_p", ctypes.c_double), ("top_k", c_i32)]
 
+    def __init__(self, temperature=0.0, top_p=0.0, min_p=0.0, top_k=0):
+        if not -1 << 31 <= top_k < 1 << 31:  # (ctypes would keep the low bits)
+            raise ValueError(f"top_k: {top_k} does not fit 32 bits")
+        super().__init__(temperature, top_p, min_p, top_k)
+
 
 class Teacher(ctypes.Structure):
     """A teacher's top logits (msd_teacher)."""
