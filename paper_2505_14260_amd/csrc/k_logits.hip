@@ -15,7 +15,9 @@
 // row 32-bit (at most 2^18 logits).
 //
 // Times here are of one MI355X, on which a copy of 82 MB reads and writes 7.0 TB/s, one of
-// 2 GiB 5.0 TB/s, and the smallest launch takes 4.2 us in a row of launches.
+// 2 GiB 5.0 TB/s, a long read alone 6.9 to 7.1, and the smallest launch takes 4.2 us in a row
+// of launches.  They are means over launches in a row, over inputs in turn; "a -> b us" are
+// those before and after a step, both of the time when it was taken.
 #include <hip/hip_fp16.h>
 
 #include <type_traits>
@@ -213,7 +215,7 @@ struct HeldRow<TYPE, LB, 0> : Row<TYPE, LB> {  // too long for that
 // A row that is read once, of up to U whole tiles, AHEAD of them under way at a time, whose
 // units' largest (of each PER of them) stay in registers: they tell which few units to read
 // again.  A quarter of a held row's registers or less, so that long rows share a CU too (top
-// 128 of 1,151 x 152,064 bf16 161 us held, 114 so).
+// 128 of 1,151 x 152,064 bf16 161 -> 114 us).
 template <int TYPE, int LB, int U, int AHEAD, int PER = 1>
 struct ToppedRow : Row<TYPE, LB> {
   using Row<TYPE, LB>::Row;
@@ -716,7 +718,10 @@ MSD_DEV int choose_few(const R& row, const Tops& t, const Scale& sc, const Logit
 // that surely stay, and it lists the tokens around the estimate, among which the border
 // then has to lie.  Where it does not (rows of very many equal logits), the border is
 // found digit by digit.  Sample by top_p of 512 x 152,064 f32: 355 us with every weight in
-// a histogram of 64-bit sums, 228 with the border estimated from counts, 158 with the means.
+// a histogram of 64-bit sums -> 228 with the border estimated from counts -> 158 with the means.
+//   Where it does not: values of 16 bits far from 0 lie so far apart that a flat row's border
+// is among more equal ones than the list or `few` holds.  Of 512 x 152,064 normal logits at a
+// mean of 12 and a deviation of 1, top_p 0.9: bf16 638 us, f16 481, f32 150.
 constexpr double COUNTS_PER_T = 64;
 constexpr int PLACE_BITS = 40;  // of a bin's sum of places, in 2^-20
 constexpr int GROUP = 8;    // stretches of a wave that are summed together: a cell
@@ -1083,8 +1088,8 @@ MSD_DEV Tops read_tops(R& row, int n, Group<R::W>& g) {
 }
 
 // Filter with a small top_k: one reading of the row, its writing, and the units with one of
-// the tokens read again.  Bound by HBM: 488 x 152,064 f32, top_k 50, 593 MB in 120 us, 4.9
-// TB/s, the rate of a large copy (133 us with every unit read again).
+// the tokens read again.  Bound by HBM: 488 x 152,064 f32, top_k 50, 594 MB in 122 us, 4.9
+// TB/s, the rate of a large copy (133 -> 120 us against every unit read again).
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_filter_few(const void* logits, size_t ld, int V,
                                                       LogitsChoice how, void* out, size_t ldo,
@@ -1120,8 +1125,8 @@ __global__ __launch_bounds__(R::LB) void k_filter_few(const void* logits, size_t
 }
 
 // The same where the units' levels tell which of them to read: under min_p most hold no
-// token that stays, so that the row is read once (filter of 488 x 152,064 f32, min_p 0.02:
-// 177 us with every unit read again, 162 with levels).
+// token that stays, so that the row is read once (filter of 488 x 152,064 f32, top_p 0.98 and
+// min_p 0.02: 177 us with every unit read again -> 162 with levels).
 template <class R>
 MSD_DEV uint32_t put_leveled(const R& row, char* o, Kept k, const Bins<R::LB>& bins, const ManyLds<R::LB>& s) {
   constexpr int AHEAD = 4;
@@ -1158,8 +1163,8 @@ MSD_DEV uint32_t put_leveled(const R& row, char* o, Kept k, const Bins<R::LB>& b
 // in it.  Many rows are bound by HBM and by the weights' arithmetic, which the two rows of a
 // CU overlap in part: 488 x 152,064 f32, min_p 0.02 and top_p 0.98, 164 us, 3.6 TB/s of what
 // has to move (119 us at a copy's rate); 27 x 32,000 f32 25 us, of one CU's arithmetic on a
-// row (at the instructions' rates 7 us of weights and 2 of counts) and the chain of barriers
-// between them.
+// row (at the instructions' rates 7 us of weights and 2 of counts) and a chain with 17
+// barriers: 27 x 8,200 takes 17 us, and 1,000 more logits 0.4.
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_filter_many(const void* logits, size_t ld, int V,
                                                        LogitsChoice how, void* out, size_t ldo,
@@ -1269,9 +1274,10 @@ __global__ __launch_bounds__(R::LB) void k_sample_few(const void* logits, size_t
 // sums of 2,048 or 4,096 neighbouring ids (a cell) tell where to read again for the draw;
 // without top_p a pass for the largest and one for the weights.  Rows are in runs, not in
 // tiles, so that a wave's cell is of neighbouring ids.  Bound by the arithmetic of the
-// weights with the first pass's HBM time not hidden by it: 512 x 152,064 f32, top_p 0.95, 148
-// us (62 us for its bytes once at a copy's rate; about 70 us for 78 million weights on 256
-// CUs at the instructions' rates).  A row alone: 1 x 32,000 f32 without a choice 13 us.
+// weights with the first pass's HBM time not hidden by it: 512 x 152,064 f32, top_p 0.95, 150
+// us (62 us for its bytes once at a copy's rate, 44 at a read's; about 70 us for 78 million
+// weights on 256 CUs at the instructions' rates).  A row alone: 1 x 32,000 f32 without a choice
+// 13 to 15 us, by its inputs.
 //   Few rows take one CU each all the same (8 x 152,064 f32, top_p: 71 us); a row over several
 // workgroups would need memory of the caller's and two more launches or a grid's barrier.
 template <class R>
@@ -1385,9 +1391,11 @@ MSD_DEV double row_sum(const Online& o, float m, float c, Group<W>& g) {
 
 // Top: one reading of the row, with its log-sum-exp (32-bit sums a thread, 64-bit over the
 // row), and the ranking.  Many rows are bound by HBM: 1,151 x 152,064 bf16, k 128, 350 MB in
-// 105 us, 3.3 TB/s, two rows to a CU, of which the ranking of one hides behind the reading of
-// the other in part; 639 x 32,000 f32, k 64, 82 MB in 23 us.  Few rows by the chain: 61 x
-// 50,021 f16, k 200, 15 us; 1 x 32,000 f32 8 us.
+// 106 us, 3.3 TB/s, two rows to a CU (103 registers; fewer maxima a thread, for three, have
+// not been tried), of which the ranking of one hides behind the reading of the other in part;
+// 639 x 32,000 f32, k 64, 82 MB in 23 us, all rows resident, three to a CU at most: about 6 us
+// of chain, then 4.3 TB/s (k 1 takes 1.5 us less).  Few rows by the chain: 61 x 50,021 f16, k
+// 200, 15 us; 1 x 32,000 f32 8 us.
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_top(const void* logits, size_t ld, int V, int n,
                                                float* values, int* ids, float* lse) {
@@ -1455,9 +1463,9 @@ struct Chains {
 // before it rounds: no second write, no atomics on the output.  Sums and weights in 32 bits
 // within a thread, in 64 over the row (a weight below 2^-126 of the largest is 0); the
 // gradient recomputes its sum, since a row is held anyway.  Bound by HBM: 639 x 32,000 f32
-// 164 MB in 43 us (3.8 TB/s: 639 rows are 512 and a tail of 127), 1,151 x 152,064 bf16 700
-// MB in 173 us (4.0 TB/s: a row to a CU, whose registers it fills, 4.5 rounds), the loss
-// alone 65 us (5.4 TB/s).
+// 164 MB in 43 us (3.8 TB/s: two rows to a CU, so 639 are 512 and a tail of 127), 1,151 x
+// 152,064 bf16 700 MB in 183 us (3.8 TB/s: a row to a CU, whose registers it fills, 4.5
+// rounds), the loss alone 66 us (5.3 TB/s).
 template <class R>
 __global__ __launch_bounds__(R::LB) void k_distill(const void* logits, size_t ld, int V,
                                                    LogitsTeacher t, float* loss, float* lse,
@@ -1559,8 +1567,8 @@ struct Tag {
 // Rows of up to this many bytes take a workgroup of 256 threads: several share a CU, and a
 // row has as few barriers' waits.  Against 1024 threads, us: top 64 of 3,000 x 1,000 f32 20
 // (89) and of 3,000 x 8,192 32 (79), filter by top_p 41 (133) and 82 (180), sample by top_p
-// of 3,000 x 1,000 47 (157), gradients 23 (109) and 43 (122).  Of 61 rows of 8,192: top 8.9
-// (9.3), filter 18.4 (17.0), gradient 14.3 (12.6).
+// of 3,000 x 1,000 47 (157), gradients 23 (109) and 43 (122).  Of 61 rows of 8,192, for which
+// the rule is the same: top 8.9 (9.3), filter 18.4 (17.0), gradient 14.3 (12.6).
 constexpr int SHORT_ROW = 256 * 8 * 16;
 
 template <class R>
@@ -1570,7 +1578,7 @@ bool holds(int cols) {
 
 // Calls f with the type for a row of `cols` that is held: by 256 threads if it is short; by
 // 512, two rows to a CU, where there are more rows than CUs (639 x 32,000 f32 43 us, by 1024
-// 50); by 1024; or read from memory in every pass, where no registers hold it.  A long row
+// 49); by 1024; or read from memory in every pass, where no registers hold it.  A long row
 // of 18 units that is read twice instead of held is no slower (1,151 x 152,064 bf16, 250 us
 // for 248 in two calls) but reads half as much again.
 template <int TYPE, class F>
@@ -1587,8 +1595,8 @@ void by_held(int rows, int cols, F f) {
 }
 
 // The same of rows that keep their units' largest.  512 threads against 1024 where there are
-// more rows than CUs: 639 x 32,000 f32 24.9 us (31.5), 300 x 32,000 16.4 (20.5), 1,151 x
-// 152,064 bf16 115 (119).
+// more rows than CUs: 639 x 32,000 f32 23.5 us (29.8), 300 x 32,000 15.5 (19.3), 1,151 x
+// 152,064 bf16 106 (114).
 template <int TYPE, class F>
 void by_tops(int rows, int cols, int k, F f) {
   constexpr int MOST = LOGITS_MAX_COLS / (1024 * Type<TYPE>::E);
@@ -1611,8 +1619,9 @@ void by_tops(int rows, int cols, int k, F f) {
 }
 
 // The same of rows that take any number of tokens: 512 threads against 1024 where there are
-// more rows than CUs: sample by top_p of 640 x 32,000 f32 71 us (95), of 512 x 152,064 158
-// (174); filter of 488 x 152,064 165 (157).
+// more rows than CUs: sample by top_p of 640 x 32,000 f32 70 us (94), of 512 x 152,064 152
+// (168); filter by top_p of 640 x 32,000 66 (83), of 488 x 152,064 176 (193), by min_p 127
+// (129), but by both, where levels spare a reading, 162 (151).
 template <int TYPE, class F>
 void by_runs(int rows, int cols, F f) {
   if (cols * Type<TYPE>::SIZE <= SHORT_ROW)
@@ -1683,8 +1692,8 @@ void launch_logits_distill(const void* x, int type, size_t ld, int rows, int col
       using R = typename decltype(r)::type;
       k_distill<R><<<rows, R::LB, 0, st>>>(x, ld, cols, t_, loss, lse, grad, dx, ldd);
     };
-    // without a gradient a row is read once, and need not be held (1,151 x 152,064 bf16 65
-    // us; both calls of the pair 246, with 1024 threads and held rows 288)
+    // without a gradient a row is read once, and need not be held (1,151 x 152,064 bf16 66
+    // us, with 1024 threads and held rows 104)
     if (!dx && rows > 256 && cols * Type<t()>::SIZE > SHORT_ROW)
       run(Tag<HeldRow<t(), 512, 0>>());
     else
